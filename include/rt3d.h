@@ -340,6 +340,86 @@ rt3d_status rt3d_kgs_reweight(const float* norms, int64_t count, float eps, floa
 rt3d_status rt3d_kgs_expand_mask(const uint8_t* group_mask, int M, int N, int Kt, int Kh, int Kw, int g_m, int g_n,
                                  uint8_t* mask, void* stream);
 
+/*
+ * 4-bit weights with group scales, for the layers that pruning leaves dense: the fully connected layers behind the convolutions
+ * of a network (Section 5's models end in them), which with one clip or a few are bound by the bytes of their weights.
+ * A filter's inputs fall into groups of `group`; weight (i, k) stands for (code - zero) * scale with its group's scale (bf16) and
+ * zero point (8 where `zeros` is NULL).  All arrays DEVICE, caller-owned, 16-byte aligned.  Layout: tiles of 16 filters x 64
+ * inputs, 512 bytes each, [ceil(m/16)][ceil(k/64)] of them; in a tile the 16 bytes at 16 (4 g + t), g < 8, t < 4, are four
+ * little-endian words: filter g, filter g + 8 (inputs 8 t .. 8 t + 7 of the tile), and the same filters with inputs 32 further on.
+ * Input e < 8 of a word is at bits 4 ((e >> 1) + 4 (e & 1)) .. + 3.  Codes of filters or inputs that do not exist are written as the
+ * zero point (8 for filters) and never reach a result.  Scales and zero points: [ceil(m/16)][ceil(k/group)][16].
+ */
+typedef struct {
+  int32_t m, k;          /* filters (outputs), inputs                                            */
+  int32_t group;         /* 32, 64 or 128                                                        */
+  uint8_t* codes;        /* rt3d_w4_codes_bytes                                                  */
+  uint16_t* scales;      /* rt3d_w4_scale_count bf16 values                                      */
+  uint8_t* zeros;        /* as many zero points (0..15), or NULL                                 */
+} rt3d_w4;
+
+/* Bytes of the codes and number of scales (and of zero points); -1 for extents that rt3d_w4_quantize refuses. */
+int64_t rt3d_w4_codes_bytes(int m, int k);
+int64_t rt3d_w4_scale_count(int m, int k, int group);
+
+/* rt3d_w4_quantize - fills q->codes, q->scales (and q->zeros) from w, device, q->m rows of q->k values `pitch` apart, RT3D_F32 or
+ * RT3D_BF16.  Of a group with values v (places behind the last input count as 0):
+ *   without zero points  scale = bf16(max |v| / 7),                    zero = 8
+ *   with                 scale = bf16((max(v, 0) - min(v, 0)) / 15),   zero = min(max(rint(-min(v, 0) / scale), 0), 15)
+ *   code = min(max(rint(v / scale) + zero, 0), 15)                     rint: ties to even; divisions in fp32
+ * A group whose scale is 0 gets zero = 8 and code = 8; one that holds an infinity or a NaN, or whose scale overflows, gets the
+ * scale NaN and zero = code = 8: products with it are NaN.
+ * rt3d_w4_unpack - the inverse: w[i][k] = (code - zero) * scale, RT3D_F32 (exact) or RT3D_BF16 (rounded).
+ * rt3d_linear_w4 - y = act(x W^T + bias): x, y device tensors of the same n, t, h, w and dtype, x->c == q->k, y->c == q->m; every
+ * voxel is a row.  bias device [m] float or NULL; relu nonzero: y = max(y, 0).  Codes enter the products as whole numbers
+ * and a group's sum is multiplied by its scale, all in fp32: nothing is rounded but the sums, and bf16 outputs once at the end.
+ * What x holds behind its last channel does not matter; y's padding channels are left as they are.  The result of a row
+ * does not depend on timing; it may depend, within rounding, on how many rows the call has.
+ * All enqueue on `stream`, allocate nothing and do not synchronise.  Errors: INVALID_ARG, SHAPE, UNSUPPORTED (a device that
+ * is not of compute capability 10.x; 2^31 rows or code tiles and more), CUDA. */
+rt3d_status rt3d_w4_quantize(const void* w, int dtype, int64_t pitch, const rt3d_w4* q, void* stream);
+rt3d_status rt3d_w4_unpack(const rt3d_w4* q, int dtype, void* w, int64_t pitch, void* stream);
+rt3d_status rt3d_linear_w4(const rt3d_tensor* x, const rt3d_w4* q, const float* bias, int relu, rt3d_tensor* y, void* stream);
+
+/*
+ * Orthogonalised updates: the step that retrains a layer's weights, the neighbour of the pruning step above (the paper trains the
+ * pruned network on under its mask, Section 4).  All pointers DEVICE unless said otherwise; weights [M][N][Kt][Kh][Kw] are an m x k
+ * matrix, m = M, k = N*Kt*Kh*Kw.
+ * rt3d_orthogonalize: out = O(g), the Newton-Schulz approximation of the nearest (semi-)orthogonal matrix: with X the
+ *   m x k matrix g / (|g| + eps) (|g| the Frobenius norm; transposed where m > k), `steps` times
+ *       X <- a X + (b A + c A A) X,   A = X X^T.
+ *   g RT3D_F32 or RT3D_BF16, rows g_pitch values apart; out bf16, rows out_pitch values apart, may not overlap g.
+ * rt3d_ortho_update: one optimiser step, everything m x k and contiguous; g RT3D_F32 or RT3D_BF16, w, momentum float:
+ *       momentum <- mask (mu momentum + g),   u = nesterov ? mask g + mu momentum : momentum,
+ *       w <- mask ((1 - lr weight_decay) w - lr scale O(u)).
+ *   mask uint8 (nonzero = kept, the form of rt3d_kgs_expand_mask) or NULL; where it is zero, w and momentum become zero whatever
+ *   w, momentum and g hold there.
+ * Products take 16-bit parts of the values on the tensor cores with fp32 sums: two parts (22 bits) of every value for
+ * rt3d_ortho_update and for the small matrices of both; results are within 1e-4 |O| of the exact ones in the Frobenius norm where
+ * not rounded to bf16.  A gradient with an infinity or a NaN gives NaN (where the mask keeps anything), one of zeros gives zeros.
+ *   steps 1..16; coefs HOST [steps][3] (a, b, c of each step) or NULL for 3.4445, -4.7750, 2.0315; they must keep every singular
+ *   value of [0, 1] below 1.9 in every step and |a + b s + c s s| at most 50, else UNSUPPORTED.  eps > 0.  p NULL: 5 steps, eps 1e-7.
+ * rt3d_ortho_workspace: bytes of the workspace both calls need (16-byte aligned, caller-owned, contents of no meaning between
+ *   calls; two calls that may overlap on the GPU, or two captured graphs that may, need one each); -1 for m or k < 1 or too large.
+ * Both enqueue on `stream`, allocate nothing and do not synchronise.  The same inputs give the same bits.
+ * Errors: INVALID_ARG, WORKSPACE (too few bytes), UNSUPPORTED (compute capability other than 10.x, coefficients), CUDA.
+ */
+typedef struct {
+  int32_t steps;
+  float eps;
+  const float* coefs;    /* HOST, or NULL                                                        */
+} rt3d_ortho_params;
+typedef struct {
+  float lr, mu, weight_decay, scale;
+  int32_t nesterov;
+  rt3d_ortho_params ortho;
+} rt3d_update_params;
+int64_t rt3d_ortho_workspace(int m, int k);
+rt3d_status rt3d_orthogonalize(const void* g, int dtype, int64_t g_pitch, int m, int k, const rt3d_ortho_params* p, void* out,
+                               int64_t out_pitch, void* workspace, int64_t workspace_bytes, void* stream);
+rt3d_status rt3d_ortho_update(float* w, float* momentum, const void* g, int dtype, const uint8_t* mask, int m, int k,
+                              const rt3d_update_params* p, void* workspace, int64_t workspace_bytes, void* stream);
+
 /* rt3d_run_calls - a sequence of the compute calls above, e.g. one forward pass of a network, issued in one go: what each
  * call enqueues and returns is what the single call would, in the order given, without the caller's language between
  * them.  Stops at the first call that fails and returns its status, its index in *failed (may be NULL).
@@ -347,9 +427,10 @@ rt3d_status rt3d_kgs_expand_mask(const uint8_t* group_mask, int M, int N, int Kt
  *   RECORD / WAIT  k[0] = slot: the slot takes the lane's work so far / the lane waits for what the slot took last
  * Calls:  SPARSE, DENSE (x, w, bias, p, y); FUSED (and r = residual or data NULL, k[0..2] = pool_t/h/w); PAIR (x, w, bias,
  * p, w2, bias2, p2, r, y); MAXPOOL (x, k[0..8] = kt kh kw st sh sw pt ph pw, y); ADD (x, r = second addend, k[0] = relu, y);
- * COPY (x.data = HOST array of rt3d_copy, k[0] = its length). */
+ * COPY (x.data = HOST array of rt3d_copy, k[0] = its length); LINEAR_W4 (x, q, bias, k[0] = relu, y). */
 enum { RT3D_CALL_SPARSE = 0, RT3D_CALL_DENSE = 1, RT3D_CALL_FUSED = 2, RT3D_CALL_PAIR = 3, RT3D_CALL_MAXPOOL = 4,
-       RT3D_CALL_ADD = 5, RT3D_CALL_RECORD = 6, RT3D_CALL_WAIT = 7, RT3D_CALL_COPY = 8 };
+       RT3D_CALL_ADD = 5, RT3D_CALL_RECORD = 6, RT3D_CALL_WAIT = 7, RT3D_CALL_COPY = 8,
+       RT3D_CALL_LINEAR_W4 = 9 };
 #define RT3D_CALL_SLOTS 8
 typedef struct {
   int32_t kind, lane;
@@ -358,6 +439,7 @@ typedef struct {
   const float *bias, *bias2;
   rt3d_conv_params p, p2;
   int32_t k[9];
+  const rt3d_w4* q;      /* HOST structure, read during the call                                 */
 } rt3d_call;
 rt3d_status rt3d_run_calls(const rt3d_call* calls, int32_t n, void* const* streams, int32_t n_streams, int32_t* failed);
 

@@ -48,15 +48,30 @@ class Call(ctypes.Structure):
     """One step of rt3d_run_calls."""
     _fields_ = [("kind", ctypes.c_int32), ("lane", ctypes.c_int32), ("x", Tensor), ("y", Tensor), ("r", Tensor),
                 ("w", ctypes.c_void_p), ("w2", ctypes.c_void_p), ("bias", ctypes.c_void_p), ("bias2", ctypes.c_void_p),
-                ("p", ConvParams), ("p2", ConvParams), ("k", ctypes.c_int32 * 9)]
+                ("p", ConvParams), ("p2", ConvParams), ("k", ctypes.c_int32 * 9), ("q", ctypes.c_void_p)]
 
 
-(CALL_SPARSE, CALL_DENSE, CALL_FUSED, CALL_PAIR, CALL_MAXPOOL, CALL_ADD, CALL_RECORD, CALL_WAIT, CALL_COPY) = range(9)
+(CALL_SPARSE, CALL_DENSE, CALL_FUSED, CALL_PAIR, CALL_MAXPOOL, CALL_ADD, CALL_RECORD, CALL_WAIT, CALL_COPY,
+ CALL_LINEAR_W4) = range(10)
 CALL_SLOTS = 8
 
 
 class Copy(ctypes.Structure):
     _fields_ = [("src", ctypes.c_void_p), ("dst", ctypes.c_void_p), ("count", ctypes.c_int32)]
+
+
+class W4(ctypes.Structure):
+    _fields_ = [("m", ctypes.c_int32), ("k", ctypes.c_int32), ("group", ctypes.c_int32), ("codes", ctypes.c_void_p),
+                ("scales", ctypes.c_void_p), ("zeros", ctypes.c_void_p)]
+
+
+class OrthoParams(ctypes.Structure):
+    _fields_ = [("steps", ctypes.c_int32), ("eps", ctypes.c_float), ("coefs", ctypes.POINTER(ctypes.c_float))]
+
+
+class UpdateParams(ctypes.Structure):
+    _fields_ = [("lr", ctypes.c_float), ("mu", ctypes.c_float), ("weight_decay", ctypes.c_float), ("scale", ctypes.c_float),
+                ("nesterov", ctypes.c_int32), ("ortho", OrthoParams)]
 
 
 class Fusion(ctypes.Structure):
@@ -109,6 +124,15 @@ def _load():
     i64p = ctypes.POINTER(ctypes.c_int64)
     lib.rt3d_conv3d_cost.argtypes = [TP, vp, CP, i64p, i64p, i64p]
     lib.rt3d_conv3d_query_algo.argtypes = [TP, vp, CP, TP, ctypes.POINTER(ctypes.c_int)]
+    i64 = ctypes.c_int64
+    lib.rt3d_w4_codes_bytes.argtypes, lib.rt3d_w4_codes_bytes.restype = [i, i], i64
+    lib.rt3d_w4_scale_count.argtypes, lib.rt3d_w4_scale_count.restype = [i, i, i], i64
+    lib.rt3d_w4_quantize.argtypes = [vp, i, i64, ctypes.POINTER(W4), vp]
+    lib.rt3d_w4_unpack.argtypes = [ctypes.POINTER(W4), i, vp, i64, vp]
+    lib.rt3d_linear_w4.argtypes = [TP, ctypes.POINTER(W4), vp, i, TP, vp]
+    lib.rt3d_ortho_workspace.argtypes, lib.rt3d_ortho_workspace.restype = [i, i], i64
+    lib.rt3d_orthogonalize.argtypes = [vp, i, i64, i, i, ctypes.POINTER(OrthoParams), vp, i64, vp, i64, vp]
+    lib.rt3d_ortho_update.argtypes = [vp, vp, vp, i, vp, i, i, ctypes.POINTER(UpdateParams), vp, i64, vp]
     lib.rt3d_last_plan.argtypes = [ctypes.POINTER(PlanInfo)]
     lib.rt3d_last_device_status.argtypes = [vp]
     lib.rt3d_launch_count.restype = ctypes.c_int64
@@ -398,6 +422,17 @@ class CallSequence:
         self.keep.append((arr, copies))
         self.calls.append(c)
 
+    def note_w4(self, stream, x, y, q, bias, relu):
+        c = Call(kind=CALL_LINEAR_W4, lane=self._lane(stream), x=x, y=y, q=ctypes.addressof(q.desc))
+        c.k[0] = int(bool(relu))
+        for t in (q.codes, q.scales, q.zeros, bias):
+            if t is not None:
+                self.biases[id(t)] = (t, t.data_ptr())
+        if bias is not None:
+            c.bias = bias.data_ptr()
+        self.keep.append(q)
+        self.calls.append(c)
+
     def note_event(self, kind, stream, event):
         """Work recorded into / waited for through a torch event, on a torch stream."""
         if kind == CALL_RECORD:
@@ -547,6 +582,129 @@ def rt3d_kgs_expand_mask(group_mask, M, N, Kt, Kh, Kw, g_m, g_n, mask, stream=No
     """group_mask: uint8 device [P,Q,Ks]; mask: uint8 device [M,N,Kt,Kh,Kw] (output)."""
     _check((_pycall_module or pycall()).expand_mask(ADDRESS["rt3d_kgs_expand_mask"], group_mask, int(M), int(N), int(Kt), int(Kh),
                                                     int(Kw), int(g_m), int(g_n), mask, stream), "rt3d_kgs_expand_mask")
+
+
+# ---------------------------------------------------------------------------------------------- 4-bit weights
+def _dtype_code(t) -> int:
+    import torch
+    try:
+        return {torch.float32: RT3D_F32, torch.bfloat16: RT3D_BF16}[t.dtype]
+    except KeyError:
+        raise ValueError(f"expected float32 or bfloat16, got {t.dtype}") from None
+
+
+def _matrix(t, m: int, k: int):
+    """(address, dtype, pitch) of a device tensor [m][k] (or [m][...] with k values each) whose rows are contiguous."""
+    if t.dim() < 2 or t.shape[0] != m or t[0].numel() != k or not t[0].is_contiguous():
+        raise ValueError(f"expected {m} contiguous rows of {k} values")
+    pitch = t.stride(0) if m > 1 else max(k, t.stride(0))
+    return t.data_ptr(), _dtype_code(t), pitch
+
+
+def rt3d_w4_codes_bytes(m: int, k: int) -> int:
+    return int(_lib.rt3d_w4_codes_bytes(int(m), int(k)))
+
+
+def rt3d_w4_scale_count(m: int, k: int, group: int) -> int:
+    return int(_lib.rt3d_w4_scale_count(int(m), int(k), int(group)))
+
+
+class W4Weights:
+    """4-bit weights of m filters with k inputs on the device: codes (uint8), scales (bfloat16) and zero points (uint8, or
+    None), in the layout of include/rt3d.h.  Allocated here where they are not given; `zeros`: the tensor, or True to allocate it."""
+
+    def __init__(self, m: int, k: int, group: int = 128, codes=None, scales=None, zeros=None, device="cuda"):
+        import torch
+        n_bytes, n_scales = rt3d_w4_codes_bytes(m, k), rt3d_w4_scale_count(m, k, group)
+        if n_bytes < 0 or n_scales < 0:
+            raise Rt3dError(ERR_INVALID_ARG, "W4Weights")
+        self.m, self.k, self.group = int(m), int(k), int(group)
+        self.codes = torch.empty(n_bytes, dtype=torch.uint8, device=device) if codes is None else codes
+        device = self.codes.device
+        tiles = (-(-self.m // 16), -(-self.k // self.group), 16)
+        self.scales = torch.empty(tiles, dtype=torch.bfloat16, device=device) if scales is None else scales
+        self.zeros = torch.empty(tiles, dtype=torch.uint8, device=device) if zeros is True else zeros or None if isinstance(zeros, bool) else zeros
+        for name, t, dtype, count in (("codes", self.codes, torch.uint8, n_bytes), ("scales", self.scales, torch.bfloat16, n_scales),
+                                      ("zeros", self.zeros, torch.uint8, n_scales)):
+            if t is not None and (t.dtype != dtype or t.numel() != count or not t.is_contiguous() or t.device != device):
+                raise ValueError(f"{name}: {count} contiguous values of {dtype} on {device} wanted")
+        self.desc = W4(self.m, self.k, self.group, self.codes.data_ptr(), self.scales.data_ptr(),
+                       None if self.zeros is None else self.zeros.data_ptr())
+
+
+def rt3d_w4_quantize(w, q: W4Weights, stream=None):
+    """w: device tensor [m][k] or [m][N][Kt][Kh][Kw], float32 or bfloat16, rows contiguous (any row pitch); fills q."""
+    ptr, dtype, pitch = _matrix(w, q.m, q.k)
+    _check(_lib.rt3d_w4_quantize(ptr, dtype, pitch, ctypes.byref(q.desc), _stream_ptr(stream)), "rt3d_w4_quantize")
+
+
+def rt3d_w4_unpack(q: W4Weights, w, stream=None):
+    """w: device tensor as for rt3d_w4_quantize (output): the values that the codes stand for."""
+    ptr, dtype, pitch = _matrix(w, q.m, q.k)
+    _check(_lib.rt3d_w4_unpack(ctypes.byref(q.desc), dtype, ptr, pitch, _stream_ptr(stream)), "rt3d_w4_unpack")
+
+
+def rt3d_linear_w4(x, q: W4Weights, bias, y, relu=False, stream=None):
+    """y = act(x W^T + bias): x, y device tensors [n,t,h,w,pitch] (or Tensor descriptors) with q.k and q.m channels, bias float32
+    device tensor [m] or None."""
+    xd = x if isinstance(x, Tensor) else tensor_desc(x, q.k)
+    yd = y if isinstance(y, Tensor) else tensor_desc(y, q.m)
+    _check(_lib.rt3d_linear_w4(ctypes.byref(xd), ctypes.byref(q.desc), _bias_ptr(bias), int(bool(relu)), ctypes.byref(yd),
+                               _stream_ptr(stream)), "rt3d_linear_w4")
+    seq = noting()
+    if seq is not None:
+        seq.note_w4(stream, xd, yd, q, bias, relu)
+
+
+# ---------------------------------------------------------------------------------------- orthogonalised updates
+def rt3d_ortho_workspace(m: int, k: int) -> int:
+    """Bytes of the workspace that rt3d_orthogonalize and rt3d_ortho_update need for an m x k matrix."""
+    return int(_lib.rt3d_ortho_workspace(int(m), int(k)))
+
+
+def _ortho_params(steps, eps, coefs) -> OrthoParams:
+    p = OrthoParams(int(steps), float(eps), None)
+    if coefs is not None:
+        flat = [float(v) for abc in coefs for v in abc]
+        if len(flat) != 3 * int(steps):
+            raise ValueError("coefs: three values for each step")
+        p.coefs = (ctypes.c_float * len(flat))(*flat)
+    return p
+
+
+def _workspace_bytes(t) -> int:
+    if not t.is_contiguous():
+        raise ValueError("the workspace must be contiguous")
+    return t.numel() * t.element_size()
+
+
+def rt3d_orthogonalize(g, out, workspace, steps: int = 5, eps: float = 1e-7, coefs=None, stream=None):
+    """g: float32 or bfloat16 device tensor [m][k] or [m][N][Kt][Kh][Kw]; out: bfloat16 of the same extents (rows contiguous, any
+    row pitch); workspace: device tensor of at least rt3d_ortho_workspace(m, k) bytes; coefs: (a, b, c) of each step or None."""
+    import torch
+    m, k = g.shape[0], g[0].numel()
+    src, dtype, g_pitch = _matrix(g, m, k)
+    dst, _, out_pitch = _matrix(out, m, k)
+    if out.dtype != torch.bfloat16:
+        raise ValueError("out must be bfloat16")
+    p = _ortho_params(steps, eps, coefs)
+    _check(_lib.rt3d_orthogonalize(src, dtype, g_pitch, m, k, ctypes.byref(p), dst, out_pitch, workspace.data_ptr(),
+                                   _workspace_bytes(workspace), _stream_ptr(stream)), "rt3d_orthogonalize")
+
+
+def rt3d_ortho_update(w, momentum, g, mask, workspace, lr: float, momentum_factor: float = 0.95, nesterov: bool = True,
+                      weight_decay: float = 0.0, scale: float = 1.0, steps: int = 5, eps: float = 1e-7, coefs=None, stream=None):
+    """One optimiser step on w (float32, in place) with momentum (float32, in place), g (float32 or bfloat16) and mask (uint8 or
+    None), contiguous device tensors of equal extents."""
+    import torch
+    m, k = w.shape[0], w[0].numel()
+    for name, t, dtype in (("w", w, torch.float32), ("momentum", momentum, torch.float32), ("g", g, g.dtype), ("mask", mask, torch.uint8)):
+        if t is not None and (t.shape != w.shape or t.dtype != dtype or not t.is_contiguous()):
+            raise ValueError(f"{name}: contiguous values of {dtype} with the weights' extents wanted")
+    p = UpdateParams(float(lr), float(momentum_factor), float(weight_decay), float(scale), int(bool(nesterov)), _ortho_params(steps, eps, coefs))
+    _check(_lib.rt3d_ortho_update(w.data_ptr(), momentum.data_ptr(), g.data_ptr(), _dtype_code(g), None if mask is None else mask.data_ptr(),
+                                  m, k, ctypes.byref(p), workspace.data_ptr(), _workspace_bytes(workspace), _stream_ptr(stream)),
+           "rt3d_ortho_update")
 
 
 def rt3d_conv3d_cost(x: Tensor, w: Packed, stride=(1, 1, 1), pad=(0, 0, 0)):

@@ -1520,6 +1520,24 @@ rt3d_status conv2plus1d_impl(const rt3d_tensor* x, const rt3d_packed* ws, const 
 #define RT3D_NOALLOC_PARTIAL_TILES 128                                   /* 128 x 256 fp32 each */
 #define RT3D_NOALLOC_PARTIAL_BYTES (RT3D_NOALLOC_PARTIAL_TILES * 128 * 256 * 4)   /* 16 MiB */
 
+namespace rt3d {
+
+bool plan_only() { return t_plan_only; }
+void count_launches(int n) { g_launches.fetch_add(n); }
+rt3d_status check_device_tensor(const rt3d_tensor* t) {
+  const rt3d_status s = check_tensor(t);
+  return s != RT3D_OK ? s : check_alignment(t);
+}
+bool tensors_overlap(const rt3d_tensor* a, const rt3d_tensor* b) { return overlaps(a, b); }
+rt3d_status current_device_info(DeviceInfo* info) {
+  DeviceState* d = nullptr;
+  const rt3d_status s = get_device_state(&d);
+  if (s == RT3D_OK) *info = {d->sm_count, d->cc_major, d->sched + 2};
+  return s;
+}
+
+}  // namespace rt3d
+
 extern "C" {
 
 rt3d_status rt3d_conv2plus1d_fused(const rt3d_tensor* x, const rt3d_packed* w_s, const float* bias_s,
@@ -1806,6 +1824,7 @@ rt3d_status rt3d_run_calls(const rt3d_call* calls, int32_t n, void* const* strea
           s = rt3d_maxpool3d(&c.x, c.k[0], c.k[1], c.k[2], c.k[3], c.k[4], c.k[5], c.k[6], c.k[7], c.k[8], &y, st);
           break;
         case RT3D_CALL_ADD: s = rt3d_add_relu(&c.x, &c.r, c.k[0], &y, st); break;
+        case RT3D_CALL_LINEAR_W4: s = c.q ? rt3d_linear_w4(&c.x, c.q, c.bias, c.k[0], &y, st) : RT3D_ERR_INVALID_ARG; break;
         case RT3D_CALL_COPY: s = rt3d_copy_f32(static_cast<const rt3d_copy*>(c.x.data), c.k[0], st); break;
         case RT3D_CALL_RECORD:
         case RT3D_CALL_WAIT: {

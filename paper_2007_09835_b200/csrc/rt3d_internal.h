@@ -229,4 +229,12 @@ const SmallCLayout* get_smallc_layout(rt3d_packed* p, int sh, int sw, bool packe
 bool f32_layout_possible(const rt3d_packed* p);
 const F32Layout* get_f32_layout(rt3d_packed* p);
 
+// What the translation units with entry points of their own (w4.cu, ortho.cu) share with api.cu.
+bool plan_only();                                         // this thread is between rt3d_plan_begin and rt3d_plan_end
+void count_launches(int n);                               // for rt3d_launch_count
+rt3d_status check_device_tensor(const rt3d_tensor* t);    // extents, dtype, pitch and alignment
+bool tensors_overlap(const rt3d_tensor* a, const rt3d_tensor* b);
+struct DeviceInfo { int sm_count, cc_major; int32_t* err; };      // err: the device's word for waits that gave up
+rt3d_status current_device_info(DeviceInfo* info);
+
 }  // namespace rt3d

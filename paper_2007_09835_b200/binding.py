@@ -152,7 +152,7 @@ _lib = _load()
 
 ADDRESS = {fn: ctypes.cast(getattr(_lib, fn), ctypes.c_void_p).value
            for fn in ("rt3d_conv3d_sparse", "rt3d_conv3d_dense", "rt3d_conv3d_sparse_fused", "rt3d_kgs_group_norms",
-                      "rt3d_kgs_reweight", "rt3d_kgs_expand_mask")}
+                      "rt3d_kgs_reweight", "rt3d_kgs_expand_mask", "rt3d_linear_w4")}
 _pycall_module = None
 
 
@@ -647,11 +647,16 @@ def rt3d_w4_unpack(q: W4Weights, w, stream=None):
 def rt3d_linear_w4(x, q: W4Weights, bias, y, relu=False, stream=None):
     """y = act(x W^T + bias): x, y device tensors [n,t,h,w,pitch] (or Tensor descriptors) with q.k and q.m channels, bias float32
     device tensor [m] or None."""
+    seq = noting()
+    if seq is None and not isinstance(x, Tensor) and not isinstance(y, Tensor):
+        status = (_pycall_module or pycall()).linear_w4(ADDRESS["rt3d_linear_w4"], x, q.desc, bias, y, relu, stream)
+        if status != OK:
+            raise Rt3dError(status, "rt3d_linear_w4")
+        return
     xd = x if isinstance(x, Tensor) else tensor_desc(x, q.k)
     yd = y if isinstance(y, Tensor) else tensor_desc(y, q.m)
     _check(_lib.rt3d_linear_w4(ctypes.byref(xd), ctypes.byref(q.desc), _bias_ptr(bias), int(bool(relu)), ctypes.byref(yd),
                                _stream_ptr(stream)), "rt3d_linear_w4")
-    seq = noting()
     if seq is not None:
         seq.note_w4(stream, xd, yd, q, bias, relu)
 

@@ -244,6 +244,34 @@ PyObject* conv(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+// A structure of the binding (ctypes) by the bytes that it holds.
+template <typename S>
+bool structure(PyObject* v, S* out) {
+  Py_buffer p;
+  if (PyObject_GetBuffer(v, &p, PyBUF_SIMPLE) != 0) return false;
+  const bool ok = p.len == Py_ssize_t(sizeof(S));
+  if (ok) __builtin_memcpy(out, p.buf, sizeof(S));
+  else PyErr_SetString(PyExc_ValueError, "not the structure that is wanted");
+  PyBuffer_Release(&p);
+  return ok;
+}
+
+// linear_w4(address, x, weights, bias, y, relu, stream) -> status
+PyObject* linear_w4(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  uintptr_t fn, bias, stream;
+  rt3d_tensor x{}, y{};
+  rt3d_w4 q;
+  if (!want(n, 7) || !as_pointer(a[0], &fn) || !structure(a[2], &q) || !tensor_or_none(a[3], &bias)) return nullptr;
+  PyObject *k = PyLong_FromLong(q.k), *m = PyLong_FromLong(q.m);
+  const bool ok = k && m && describe(a[1], k, &x) && describe(a[4], m, &y);
+  Py_XDECREF(k); Py_XDECREF(m);
+  const int relu = ok ? PyObject_IsTrue(a[5]) : -1;
+  if (relu < 0 || !stream_of(a[6], &stream)) return nullptr;
+  return released([&] {
+    return reinterpret_cast<decltype(&rt3d_linear_w4)>(fn)(&x, &q, reinterpret_cast<const float*>(bias), relu, &y, reinterpret_cast<void*>(stream));
+  });
+}
+
 PyMethodDef methods[] = {
     {"setup", setup, METH_VARARGS, "setup(float32, bfloat16, raw_stream, get_device): torch objects the calls need"},
     {"conv", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(conv)), METH_FASTCALL,
@@ -251,6 +279,8 @@ PyMethodDef methods[] = {
     {"group_norms", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(group_norms)), METH_FASTCALL, ""},
     {"reweight", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(reweight)), METH_FASTCALL, ""},
     {"expand_mask", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(expand_mask)), METH_FASTCALL, ""},
+    {"linear_w4", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(linear_w4)), METH_FASTCALL,
+     "linear_w4(address, x, weights, bias, y, relu, stream) -> status"},
     {"pointers_are", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(pointers_are)), METH_FASTCALL,
      "pointers_are(tensors, addresses) -> bool"},
     {nullptr, nullptr, 0, nullptr}};

@@ -2,6 +2,7 @@
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
+#include <atomic>
 #include <cstdint>
 
 #include "pdl.cuh"
@@ -25,17 +26,10 @@ __device__ __forceinline__ float ld_cluster_f32(uint32_t addr) {
 // max(v, 0) that lets a NaN through.
 __device__ __forceinline__ float relu_of(float v) { return v < 0.f ? 0.f : v; }
 
-__device__ __forceinline__ float value_of(const float* p) { return *p; }
-__device__ __forceinline__ float value_of(const __nv_bfloat16* p) { return __bfloat162float(*p); }
 __device__ __forceinline__ void store_value(float* p, float v) { *p = v; }
 __device__ __forceinline__ void store_value(__nv_bfloat16* p, float v) { *p = __float2bfloat16_rn(v); }
 __device__ __forceinline__ float bf16_float(uint16_t b) { return __uint_as_float(uint32_t(b) << 16); }
 
-// Words of the code layout: filter i (of all), input block of 8 kw -> word index; shift of input e inside the word.
-__device__ __forceinline__ long long word_of(int i, int kw, int k_blocks) {
-  const int r = i & 15, b = kw >> 3, t = kw & 3, half = (kw >> 2) & 1;
-  return ((long long)(i >> 4) * k_blocks + b) * 128 + ((r & 7) * 4 + t) * 4 + half * 2 + (r >> 3);
-}
 __device__ __forceinline__ int shift_of(int e) { return 4 * ((e >> 1) + 4 * (e & 1)); }
 
 // Scale, zero point and codes of a group as include/rt3d.h defines them.
@@ -52,58 +46,177 @@ __device__ __forceinline__ Grid grid_of(float low, float high, bool bad, bool ze
   q.zero = zeros && q.scale > 0.f ? fminf(fmaxf(rintf(__fdiv_rn(-low, q.scale)), 0.f), 15.f) : 8.f;
   return q;
 }
-__device__ __forceinline__ uint32_t code_of(float v, const Grid& q) {
-  if (!(q.scale > 0.f)) return 8u;
-  return uint32_t(fminf(fmaxf(rintf(__fdiv_rn(v, q.scale)) + q.zero, 0.f), 15.f));
+// A quotient decides between two codes only next to a half: elsewhere the product with the rounded reciprocal, off by less than
+// 2^-19 of quotients up to 16, gives the same code.  (4096 x 8192 fp32, a division for every weight: 70 us; 30 this way.)
+__device__ __forceinline__ uint32_t code_of(float v, const Grid& q, float inv) {
+  float p = v * inv, r = rintf(p);
+  if (!(fabsf(fabsf(p - r) - 0.5f) >= 1e-5f)) r = rintf(__fdiv_rn(v, q.scale));      // a NaN (reciprocal out of range) too
+  return uint32_t(fminf(fmaxf(r + q.zero, 0.f), 15.f));
 }
 
-// One thread for a group of a filter; threads of filters that do not exist write the padding of the last tile.
-template <typename T>
-__global__ void w4_quantize_kernel(const T* __restrict__ w, long long pitch, int m, int k, int group, int n_groups, int k_blocks,
-                                   uint32_t* __restrict__ codes, uint16_t* __restrict__ scales, uint8_t* __restrict__ zeros,
-                                   long long total) {
-  pdl_entry();
-  const long long idx = (long long)blockIdx.x * blockDim.x + threadIdx.x;
-  if (idx >= total) return;
-  const int g = int(idx % n_groups), i = int(idx / n_groups);
-  const int k0 = g * group, n = min(group, k - k0);
-  const T* src = w + (long long)i * pitch + k0;
-  float low = 0.f, high = 0.f;
-  bool bad = false;
-  if (i < m)
-    for (int j = 0; j < n; ++j) {
-      const float v = value_of(src + j);
-      low = fminf(low, v); high = fmaxf(high, v);
-      bad |= !(fabsf(v) < __int_as_float(0x7f800000));
-    }
-  const Grid q = grid_of(low, high, bad, zeros != nullptr);
-  const long long at = ((long long)(i >> 4) * n_groups + g) * 16 + (i & 15);
-  scales[at] = q.bits;
-  if (zeros) zeros[at] = uint8_t(q.zero);
-  const int last = g == n_groups - 1 ? k_blocks * 8 : (k0 + group) / 8;
-  for (int kw = k0 / 8; kw < last; ++kw) {
-    uint32_t word = 0;
-    for (int e = 0; e < 8; ++e) {
-      const int j = kw * 8 + e - k0;
-      word |= (i < m && j < n ? code_of(value_of(src + j), q) : uint32_t(q.zero)) << shift_of(e);
-    }
-    codes[word_of(i, kw, k_blocks)] = word;
+// Eight values of a row in memory, those from `n` on zero; kVec: on a 16-byte boundary.
+template <bool kVec>
+__device__ __forceinline__ void load8(const float* p, int n, float (&v)[8]) {
+  if (kVec && n >= 8) {
+    const float4 a = __ldg(reinterpret_cast<const float4*>(p)), b = __ldg(reinterpret_cast<const float4*>(p) + 1);
+    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+    return;
   }
+#pragma unroll
+  for (int e = 0; e < 8; ++e) v[e] = e < n ? __ldg(p + e) : 0.f;
+}
+template <bool kVec>
+__device__ __forceinline__ void load8(const __nv_bfloat16* p, int n, float (&v)[8]) {
+  if (kVec && n >= 8) {
+    const uint4 u = __ldg(reinterpret_cast<const uint4*>(p));
+    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = __uint_as_float(e & 1 ? w[e >> 1] & 0xffff0000u : w[e >> 1] << 16);
+    return;
+  }
+#pragma unroll
+  for (int e = 0; e < 8; ++e) v[e] = e < n ? __bfloat162float(p[e]) : 0.f;
+}
+template <bool kVec>
+__device__ __forceinline__ void store8(float* p, int n, const float (&v)[8]) {
+  if (kVec && n >= 8) {
+    reinterpret_cast<float4*>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
+    reinterpret_cast<float4*>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
+    return;
+  }
+#pragma unroll
+  for (int e = 0; e < 8; ++e)
+    if (e < n) p[e] = v[e];
+}
+template <bool kVec>
+__device__ __forceinline__ void store8(__nv_bfloat16* p, int n, const float (&v)[8]) {
+  if (kVec && n >= 8) {
+    uint32_t w[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const __nv_bfloat162 b = __floats2bfloat162_rn(v[2 * e], v[2 * e + 1]);
+      w[e] = *reinterpret_cast<const uint32_t*>(&b);
+    }
+    *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+    return;
+  }
+#pragma unroll
+  for (int e = 0; e < 8; ++e)
+    if (e < n) p[e] = __float2bfloat16_rn(v[e]);
 }
 
-template <typename T>
-__global__ void w4_unpack_kernel(const uint32_t* __restrict__ codes, const uint16_t* __restrict__ scales,
-                                 const uint8_t* __restrict__ zeros, int m, int k, int group, int n_groups, int k_blocks, int words,
-                                 T* __restrict__ w, long long pitch, long long total) {
+struct GridArgs {                    // of the two calls between 4-bit and plain weights
+  uint4* codes;
+  uint16_t* scales;
+  uint8_t* zeros;
+  long long pitch;
+  int m, k, n_groups, k_blocks;
+  long long chunks, total;           // of 128 inputs in a row of tiles, and in all
+};
+
+// A warp takes 128 inputs of 16 filters, whole groups: lane 4 g + t has 8 inputs of the filters g and g + 8 in each of the four
+// 32s, which are the words that it packs; four lanes make a group's extremes.  Read once, written in runs of 512 bytes.
+// kGroup32: 32s in a group.
+template <typename T, int kGroup32, bool kVec>
+__global__ void __launch_bounds__(256)
+w4_quantize_kernel(const T* __restrict__ w, const GridArgs a) {
   pdl_entry();
-  const long long idx = (long long)blockIdx.x * blockDim.x + threadIdx.x;
-  if (idx >= total) return;
-  const int kw = int(idx % words), i = int(idx / words);
-  const long long at = ((long long)(i >> 4) * n_groups + kw * 8 / group) * 16 + (i & 15);
-  const float s = bf16_float(scales[at]), z = zeros ? float(zeros[at]) : 8.f;
-  const uint32_t word = codes[word_of(i, kw, k_blocks)];
-  for (int e = 0; e < 8 && kw * 8 + e < k; ++e)
-    store_value(w + (long long)i * pitch + kw * 8 + e, (float((word >> shift_of(e)) & 15u) - z) * s);
+  const long long unit = ((long long)blockIdx.x * 256 + threadIdx.x) >> 5;
+  if (unit >= a.total) return;
+  const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+  const long long tile = unit / a.chunks;
+  const int k0 = int(unit - tile * a.chunks) * 128;
+  uint32_t words[2][4];              // filter, 32 inputs
+#pragma unroll
+  for (int f = 0; f < 2; ++f) {
+    const int i = int(tile) * 16 + g + 8 * f;
+    const T* row = w + (long long)i * a.pitch;
+    float v[4][8], low[4], high[4];
+    bool bad[4];
+    uint32_t filled = 0x88888888u;                   // the codes of values of zero
+#pragma unroll
+    for (int b = 0; b < 4; ++b) {
+      const int at = k0 + b * 32 + t * 8;
+      load8<kVec>(row + at, i < a.m ? a.k - at : 0, v[b]);
+    }
+#pragma unroll
+    for (int b = 0; b < 4; ++b) {
+      low[b] = high[b] = 0.f;
+      bad[b] = false;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        low[b] = fminf(low[b], v[b][e]); high[b] = fmaxf(high[b], v[b][e]);
+        bad[b] |= !(fabsf(v[b][e]) < __int_as_float(0x7f800000));
+      }
+#pragma unroll
+      for (int o = 1; o <= 2; o *= 2) {
+        low[b] = fminf(low[b], __shfl_xor_sync(0xffffffffu, low[b], o));
+        high[b] = fmaxf(high[b], __shfl_xor_sync(0xffffffffu, high[b], o));
+        bad[b] |= __shfl_xor_sync(0xffffffffu, int(bad[b]), o) != 0;
+      }
+    }
+#pragma unroll
+    for (int b = 0; b < 4; b += kGroup32) {
+#pragma unroll
+      for (int c = 1; c < kGroup32; ++c) {
+        low[b] = fminf(low[b], low[b + c]); high[b] = fmaxf(high[b], high[b + c]); bad[b] |= bad[b + c];
+      }
+      const Grid q = grid_of(low[b], high[b], bad[b], a.zeros != nullptr);
+      const int group = (k0 + b * 32) / (32 * kGroup32);
+      if (t == 0 && group < a.n_groups) {
+        const long long at = (tile * a.n_groups + group) * 16 + g + 8 * f;
+        a.scales[at] = q.bits;
+        if (a.zeros) a.zeros[at] = uint8_t(q.zero);
+      }
+      // places that do not exist hold zeros; behind the last group they have its zero point
+      const float inv = __fdiv_rn(1.f, q.scale);
+      if (group < a.n_groups) filled = uint32_t(q.zero) * 0x11111111u;
+#pragma unroll
+      for (int c = 0; c < kGroup32; ++c) {
+        uint32_t word = 0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) word |= code_of(v[b + c][e], q, inv) << shift_of(e);
+        words[f][b + c] = q.scale > 0.f ? word : filled;
+      }
+    }
+  }
+  uint4* dst = a.codes + (tile * a.k_blocks + k0 / 64) * 32 + lane;
+#pragma unroll
+  for (int b = 0; b < 2; ++b)
+    if (k0 / 64 + b < a.k_blocks) dst[b * 32] = make_uint4(words[0][2 * b], words[1][2 * b], words[0][2 * b + 1], words[1][2 * b + 1]);
+}
+
+template <typename T, int kGroup32, bool kVec>
+__global__ void __launch_bounds__(256)
+w4_unpack_kernel(T* __restrict__ w, const GridArgs a) {
+  pdl_entry();
+  const long long unit = ((long long)blockIdx.x * 256 + threadIdx.x) >> 5;
+  if (unit >= a.total) return;
+  const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+  const long long tile = unit / a.chunks;
+  const int k0 = int(unit - tile * a.chunks) * 128;
+  const uint4* src = a.codes + (tile * a.k_blocks + k0 / 64) * 32 + lane;
+#pragma unroll
+  for (int b = 0; b < 2; ++b) {
+    if (k0 / 64 + b >= a.k_blocks) return;
+    const uint4 u = __ldg(src + b * 32);
+    const uint32_t words[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+    for (int f = 0; f < 2; ++f) {
+      const int i = int(tile) * 16 + g + 8 * f;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int at = k0 + b * 64 + h * 32 + t * 8;
+        if (i >= a.m || at >= a.k) continue;
+        const long long s_at = (tile * a.n_groups + at / (32 * kGroup32)) * 16 + g + 8 * f;
+        const float s = bf16_float(__ldg(a.scales + s_at)), z = a.zeros ? float(__ldg(a.zeros + s_at)) : 8.f;
+        float v[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = (float((words[2 * h + f] >> shift_of(e)) & 15u) - z) * s;
+        store8<kVec>(w + (long long)i * a.pitch + at, a.k - at, v);
+      }
+    }
+  }
 }
 
 // ------------------------------------------------------------------------------------------------ products of a few rows
@@ -112,80 +225,81 @@ __global__ void w4_unpack_kernel(const uint32_t* __restrict__ codes, const uint1
 // without a rounding but the fp32 sum's, and the scale multiplies that sum in fp32.  fp32 rows go in as three bf16
 // parts that add up to the value.  16 filters are the products' rows, 8 rows of x their columns: the tile layout holds for each lane
 // the 16 bytes it needs, so a warp reads 512 bytes in a row, and nothing goes through shared memory but the sums at the end.
-// (c - z): the four bits go into the mantissa of 128 (bf16 has 7 bits), from which 128 + z is taken, exactly: 11 instructions for
-// eight weights.
+// (c - z): four bits at the bottom of a bf16 are the subnormal c 2^-133, at bits 4 to 7 (the lowest bit of the exponent among them)
+// c 2^-129: one fused multiply-add makes (c - z) / 64 of either, exactly, and the result takes the 64 back.  9 instructions for
+// eight weights, 5 of them on the integer pipe, which bounds the kernel where the codes come from the L2.
 //
 // A CTA's eight warps take every eighth block of 64 inputs of kTiles tiles of filters; where there are few tiles, the CTAs of a cluster
 // share the inputs further and add their sums up through one another's shared memory, always in the same order.
 constexpr int kLinearThreads = 256;
-constexpr uint32_t kBias128 = 0x43004300u;                  // bf16 128, twice
 
-__device__ __forceinline__ uint32_t sub_bf16x2(uint32_t a, uint32_t b) {
-  const __nv_bfloat162 d = __hsub2(*reinterpret_cast<const __nv_bfloat162*>(&a), *reinterpret_cast<const __nv_bfloat162*>(&b));
-  return *reinterpret_cast<const uint32_t*>(&d);
+__device__ __forceinline__ uint32_t fma_bf16x2(uint32_t a, uint32_t b, uint32_t c) {
+  uint32_t d;
+  asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(d) : "r"(a), "r"(b), "r"(c));
+  return d;
 }
-// Eight codes of a word as four pairs of whole numbers, inputs (2 p, 2 p + 1).
-__device__ __forceinline__ void spread_codes(uint32_t w, uint32_t zero, uint32_t (&v)[4]) {
-#pragma unroll
-  for (int p = 0; p < 4; ++p) v[p] = sub_bf16x2(((w >> (4 * p)) & 0x000F000Fu) | kBias128, zero);
+constexpr uint32_t kTwo127 = 0x7f007f00u, kTwo123 = 0x7d007d00u;               // bf16 2^127 and 2^123, twice
+constexpr uint32_t kMinusEighth = 0xbe00be00u;                                 // -8 / 64, twice
+// -z / 64, twice: 128 + z has z in its mantissa, and -(128 + z) / 64 + 2.
+__device__ __forceinline__ uint32_t minus_zero(uint32_t z) { return fma_bf16x2(z * 0x00010001u + 0x43004300u, 0xbc80bc80u, 0x40004000u); }
+// Eight codes of a word as four pairs of (code - zero) / 64, inputs (2 p, 2 p + 1).
+__device__ __forceinline__ void spread_codes(uint32_t w, uint32_t minus, uint32_t (&v)[4]) {
+  const uint32_t u = w >> 8;
+  v[0] = fma_bf16x2(w & 0x000F000Fu, kTwo127, minus);
+  v[1] = fma_bf16x2(w & 0x00F000F0u, kTwo123, minus);
+  v[2] = fma_bf16x2(u & 0x000F000Fu, kTwo127, minus);
+  v[3] = fma_bf16x2(u & 0x00F000F0u, kTwo123, minus);
 }
 __device__ __forceinline__ void mma_bf16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-               : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
-// Eight inputs of a row from k0 on as they lie in memory; zeros where there are none.
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+// The first `bytes` come from global memory, the rest of the 16 are zeros.
+__device__ __forceinline__ void copy16_part(uint32_t dst, const void* src, int bytes) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int kPending>
+__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(kPending) : "memory"); }
+// Eight inputs of a row as bf16 pairs, 512 bytes between a lane's units.
 template <typename T>
-struct Chunk;
+struct Operand;
 template <>
-struct Chunk<__nv_bfloat16> {
-  static constexpr int kParts = 1;
-  uint4 v;
-  __device__ __forceinline__ void load(const __nv_bfloat16* row, int k0, int k) {
-    v = make_uint4(0u, 0u, 0u, 0u);
-    if (!row || k0 >= k) return;
-    if (k0 + 8 <= k) { v = __ldg(reinterpret_cast<const uint4*>(row + k0)); return; }
-    uint32_t w[4] = {0u, 0u, 0u, 0u};
-#pragma unroll
-    for (int e = 0; e < 8; ++e)
-      if (k0 + e < k) w[e >> 1] |= uint32_t(__bfloat16_as_ushort(row[k0 + e])) << (16 * (e & 1));
-    v = make_uint4(w[0], w[1], w[2], w[3]);
+struct Operand<__nv_bfloat16> {
+  static constexpr int kParts = 1, kUnits = 1;
+  static __device__ __forceinline__ void read(const unsigned char* at, uint32_t (&b)[kParts][4]) {
+    const uint4 v = *reinterpret_cast<const uint4*>(at);
+    b[0][0] = v.x; b[0][1] = v.y; b[0][2] = v.z; b[0][3] = v.w;
   }
-  __device__ __forceinline__ void parts(uint32_t (&b)[kParts][4]) const { b[0][0] = v.x; b[0][1] = v.y; b[0][2] = v.z; b[0][3] = v.w; }
 };
 template <>
-struct Chunk<float> {
-  static constexpr int kParts = 3;
-  float f[8];
-  __device__ __forceinline__ void load(const float* row, int k0, int k) {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) f[e] = 0.f;
-    if (!row || k0 >= k) return;
-    if (k0 + 8 <= k) {
-      const float4 a = __ldg(reinterpret_cast<const float4*>(row + k0)), b = __ldg(reinterpret_cast<const float4*>(row + k0 + 4));
-      f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w; f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
-      return;
-    }
-#pragma unroll
-    for (int e = 0; e < 8; ++e)
-      if (k0 + e < k) f[e] = row[k0 + e];
-  }
+struct Operand<float> {
+  static constexpr int kParts = 3, kUnits = 2;
   // The upper 8 bits of the mantissa, the next 8 and the last 8: each part is the rest's leading bits, so the three add up to the
   // value and none is larger than it.  An infinity has no rest; a NaN's is a NaN.
-  __device__ __forceinline__ void parts(uint32_t (&b)[kParts][4]) const {
+  static __device__ __forceinline__ void read(const unsigned char* at, uint32_t (&b)[kParts][4]) {
 #pragma unroll
-    for (int p = 0; p < 4; ++p) {
-      uint32_t bits[3][2];
+    for (int u = 0; u < 2; ++u) {
+      const uint4 v = *reinterpret_cast<const uint4*>(at + u * 512);
+      const uint32_t f[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const float x = f[2 * p + e];
-        const uint32_t h = __float_as_uint(x) & 0xffff0000u;
-        const float r = fabsf(x) == __int_as_float(0x7f800000) ? 0.f : x - __uint_as_float(h);
-        const uint32_t m = __float_as_uint(r) & 0xffff0000u;
-        bits[0][e] = h; bits[1][e] = m; bits[2][e] = __float_as_uint(r - __uint_as_float(m));
+      for (int p = 0; p < 2; ++p) {
+        uint32_t bits[3][2];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const float x = __uint_as_float(f[2 * p + e]);
+          const uint32_t h = f[2 * p + e] & 0xffff0000u;
+          const float r = fabsf(x) == __int_as_float(0x7f800000) ? 0.f : x - __uint_as_float(h);
+          const uint32_t m = __float_as_uint(r) & 0xffff0000u;
+          bits[0][e] = h; bits[1][e] = m; bits[2][e] = __float_as_uint(r - __uint_as_float(m));
+        }
+#pragma unroll
+        for (int q = 0; q < 3; ++q) b[q][2 * u + p] = __byte_perm(bits[q][0], bits[q][1], 0x7632);
       }
-#pragma unroll
-      for (int q = 0; q < 3; ++q) b[q][p] = __byte_perm(bits[q][0], bits[q][1], 0x7632);
     }
   }
 };
@@ -202,136 +316,274 @@ struct LinearArgs {
   int rows;
 };
 
-template <typename T, int kTiles, int kRows8, bool kFine, bool kZeros>        // kFine: groups of 32, two to a block
-__global__ void __launch_bounds__(kLinearThreads, 2)
-linear_w4_kernel(const LinearArgs a) {
-  constexpr int kCols = kRows8 * 8, kOut = kTiles * 16 * kCols, kParts = Chunk<T>::kParts;
-  __shared__ __align__(16) float part[8][kOut];
-  pdl_entry();
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-  const uint32_t ranks = cluster_size(), rank = cluster_ctarank();
-  const int tile0 = int(blockIdx.x / ranks) * kTiles;
-  const long long row0 = (long long)blockIdx.y * kCols;
-  const T* rows[kRows8];
+// A stage of a warp's ring: kDeep neighbouring blocks of 64 inputs: the codes [block][tile], the rows of x [block], then the
+// groups' scales [tile][group] and zero points.
+template <typename T, int kTiles, int kRows8, bool kFine>
+struct Ring {
+  static constexpr int kDeep = sizeof(T) == 4 && kRows8 == 2 ? 1 : sizeof(T) == 2 && kTiles <= 2 && kRows8 == 1 ? 4 : 2;
+  static constexpr int kGroups = kFine ? 2 * kDeep : kDeep, kX = kRows8 * 2 * Operand<T>::kUnits;
+  static constexpr uint32_t kXBlock = kX * 512, kXAt = kDeep * kTiles * 512, kGridAt = kXAt + kDeep * kXBlock;
+  static constexpr uint32_t kZeroAt = kGridAt + kTiles * kGroups * 32;
+  static constexpr uint32_t kStage = (kZeroAt + kTiles * kGroups * 16 + 127) / 128 * 128;
+  static constexpr int kFit = int(104 * 1024 / 8 / kStage), kDepth = kFit >= 6 ? 6 : kFit >= 2 ? kFit : 2;
+  static constexpr uint32_t kSums = 8 * kTiles * 16 * kRows8 * 8 * 4, kRings = 8 * kDepth * kStage, kBytes = kRings > kSums ? kRings : kSums;
+};
+
+// Sums of kNt <= kTiles tiles from `tile0` on over this warp's stages.
+template <typename T, int kTiles, int kNt, int kRows8, bool kFine, bool kZeros>
+__device__ __forceinline__ void linear_sums(const LinearArgs& a, unsigned char* ring, int tile0, long long row0, int first, int step, int lane,
+                                            float (&acc)[kTiles][kRows8][4]) {
+  typedef Ring<T, kTiles, kRows8, kFine> R;
+  constexpr int kParts = Operand<T>::kParts, kUnits = Operand<T>::kUnits;
+  const int g = lane >> 2, t = lane & 3;
+  const int n = first < a.k_blocks ? (a.k_blocks - first + step - 1) / step : 0;   // this warp's stages
+  const int stage_groups = kFine ? 2 * R::kDeep : (R::kDeep + a.group_shift) >> a.group_shift;      // groups of a stage
+
+  // What this lane copies of a stage, as addresses that go on from stage to stage: its 16 bytes of every tile's codes, its eight
+  // inputs of rows g, g + 8, .. and up to two of the 16-byte units of the scales (two a group) and zero points (one).
+  const unsigned char* codes = reinterpret_cast<const unsigned char*>(a.codes) + ((long long)tile0 * a.k_blocks + first) * 512 + lane * 16;
+  const long long tile_step = (long long)a.k_blocks * 512;
+  const unsigned char* rows[kRows8];
 #pragma unroll
   for (int r = 0; r < kRows8; ++r)
-    rows[r] = row0 + r * 8 + g < a.rows ? static_cast<const T*>(a.x) + (row0 + r * 8 + g) * a.x_pitch : nullptr;
-
-  // One block of 64 inputs: the codes of kTiles tiles, and their scales (and zero points), of which lane 4 g + t loads filter
-  // g + 8 (t & 1) of the block's half t / 2.  Both, and bf16 rows of up to 16, are asked for a block ahead.
-  constexpr bool kAhead = sizeof(T) == 2 && kRows8 <= 2;
-  struct Block {
-    uint4 codes[kTiles];
-    uint32_t scale[kTiles], zero[kTiles];
-    Chunk<T> x[kAhead ? kRows8 : 1][2];
-  };
-  auto fetch = [&](Block& b, int kb) {
+    rows[r] = row0 + r * 8 + g < a.rows
+                  ? static_cast<const unsigned char*>(a.x) + ((row0 + r * 8 + g) * a.x_pitch + first * 64 + t * 8) * int(sizeof(T)) : nullptr;
+  constexpr int kScaleUnits = kTiles * R::kGroups * 2, kGridUnits = kScaleUnits + (kZeros ? kTiles * R::kGroups : 0);
+  constexpr int kMine = (kGridUnits + 31) / 32;
+  const unsigned char* grid[kMine];                  // nullptr: nothing
+  int grid_group[kMine];
 #pragma unroll
-    for (int i = 0; i < kTiles; ++i) {
-      const int tile = min(tile0 + i, a.n_tiles - 1);                          // a tile too many: computed and dropped
-      b.codes[i] = __ldg(a.codes + ((long long)tile * a.k_blocks + kb) * 32 + lane);
-      const int grp = min(kFine ? kb * 2 + (t >> 1) : kb >> a.group_shift, a.n_groups - 1);
-      const long long at = ((long long)tile * a.n_groups + grp) * 16 + g + 8 * (t & 1);
-      b.scale[i] = __ldg(a.scales + at);
-      if (kZeros) b.zero[i] = __ldg(a.zeros + at);
+  for (int c = 0; c < kMine; ++c) {
+    const int u = lane + 32 * c;
+    const bool z = u >= kScaleUnits;
+    const int of_tile = z ? (u - kScaleUnits) % R::kGroups : u % (2 * R::kGroups) / 2;
+    const int i = z ? (u - kScaleUnits) / R::kGroups : u / (2 * R::kGroups);
+    grid_group[c] = (kFine ? first * 2 : first >> a.group_shift) + of_tile;
+    const long long at = (long long)(tile0 + i) * a.n_groups + grid_group[c];
+    grid[c] = u >= kGridUnits || i >= kNt || of_tile >= stage_groups ? nullptr
+              : z ? a.zeros + at * 16 : reinterpret_cast<const unsigned char*>(a.scales) + at * 32 + (u & 1) * 16;
+  }
+  const int group_step = kFine ? 2 * step : step >> a.group_shift;
+  const uint32_t ring_s = smem_u32(ring) + lane * 16;
+
+  // rows that do not exist are zeros, once and for all
+#pragma unroll
+  for (int r = 0; r < kRows8; ++r)
+    if (!rows[r])
+      for (int s = 0; s < R::kDepth; ++s)
+        for (int d = 0; d < R::kDeep; ++d)
+#pragma unroll
+          for (int u = 0; u < 2 * kUnits; ++u)
+            *reinterpret_cast<uint4*>(ring + s * R::kStage + R::kXAt + d * R::kXBlock + (r * 2 * kUnits + u) * 512 + lane * 16) = make_uint4(0u, 0u, 0u, 0u);
+
+  int f_kb = first;                                  // the next stage to be copied
+  uint32_t f_at = ring_s;
+  auto fetch = [&] {
+    if (f_kb < a.k_blocks) {
+      const bool whole = (f_kb + R::kDeep) * 64 <= a.k;
+      if (whole) {
+#pragma unroll
+        for (int i = 0; i < kNt; ++i) {
+          const unsigned char* p = codes + i * tile_step;
+#pragma unroll
+          for (int d = 0; d < R::kDeep; ++d) copy16(f_at + (d * kTiles + i) * 512, p + d * 512);
+        }
+#pragma unroll
+        for (int r = 0; r < kRows8; ++r)
+          if (rows[r]) {
+#pragma unroll
+            for (int d = 0; d < R::kDeep; ++d)
+#pragma unroll
+              for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int u = 0; u < kUnits; ++u)
+                  copy16(f_at + R::kXAt + d * R::kXBlock + ((r * 2 + h) * kUnits + u) * 512, rows[r] + (d * 64 + h * 32 + u * 4) * int(sizeof(T)));
+          }
+#pragma unroll
+        for (int c = 0; c < kMine; ++c)
+          if (grid[c]) copy16(f_at + R::kGridAt + c * 512, grid[c]);
+      } else {                                       // the last one, where it ends early: what lies behind the last input is not read
+#pragma unroll 1
+        for (int d = 0; d < R::kDeep && f_kb + d < a.k_blocks; ++d) {
+#pragma unroll 1
+          for (int i = 0; i < kNt; ++i) copy16(f_at + (d * kTiles + i) * 512, codes + i * tile_step + d * 512);
+#pragma unroll
+          for (int r = 0; r < kRows8; ++r)
+            if (rows[r]) {
+#pragma unroll
+              for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int u = 0; u < kUnits; ++u) {
+                  const int in = d * 64 + h * 32 + u * 4, left = (a.k - (f_kb * 64 + in + t * 8)) * int(sizeof(T));
+                  copy16_part(f_at + R::kXAt + d * R::kXBlock + ((r * 2 + h) * kUnits + u) * 512, left > 0 ? rows[r] + in * int(sizeof(T)) : static_cast<const unsigned char*>(a.x),
+                              max(0, min(16, left)));
+                }
+            }
+        }
+#pragma unroll
+        for (int c = 0; c < kMine; ++c)
+          if (grid[c])                               // zeros for groups that do not exist
+            copy16_part(f_at + R::kGridAt + c * 512, grid_group[c] < a.n_groups ? grid[c] : static_cast<const unsigned char*>(a.x),
+                        grid_group[c] < a.n_groups ? 16 : 0);
+      }
+      f_kb += step;
+      codes += step * 512;
+#pragma unroll
+      for (int r = 0; r < kRows8; ++r)
+        if (rows[r]) rows[r] += step * 64 * int(sizeof(T));
+#pragma unroll
+      for (int c = 0; c < kMine; ++c)
+        if (grid[c]) {
+          grid_group[c] += group_step;
+          grid[c] += group_step * (lane + 32 * c >= kScaleUnits ? 16 : 32);
+        }
+      f_at = f_at + R::kStage == ring_s + R::kDepth * R::kStage ? ring_s : f_at + R::kStage;
     }
-    if constexpr (kAhead) {
+    copies_commit();
+  };
+
+  auto use = [&](const unsigned char* at, int d) {    // block d of the stage at `at`
+    const unsigned char *mine = at + d * (kTiles * 512) + lane * 16, *x_at = at + R::kXAt + d * R::kXBlock + lane * 16;
+    uint32_t xb[2][kRows8][kParts][4];
+    constexpr bool kBoth = kParts == 1 && kRows8 <= 2;                         // both halves' rows in registers at a time
+    if (kBoth) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int r = 0; r < kRows8; ++r) Operand<T>::read(x_at + (r * 2 + h) * kUnits * 512, xb[h][r]);
+    }
+    // one half of one tile: 32 inputs
+    auto half = [&](int i, int h, const uint4& w, float (&sum)[kRows8][4]) {
+      const int q = i * R::kGroups + (kFine ? 2 * d + h : d >> a.group_shift);
+      uint32_t z0 = kMinusEighth, z1 = kMinusEighth, va[4], vb[4];
+      if (kZeros) {
+        z0 = minus_zero(at[R::kZeroAt + q * 16 + g]);
+        z1 = minus_zero(at[R::kZeroAt + q * 16 + g + 8]);
+      }
+      spread_codes(h ? w.z : w.x, z0, va);
+      spread_codes(h ? w.w : w.y, z1, vb);
 #pragma unroll
       for (int r = 0; r < kRows8; ++r)
 #pragma unroll
-        for (int h = 0; h < 2; ++h) b.x[r][h].load(rows[r], kb * 64 + h * 32 + t * 8, a.k);
-    }
-  };
-
-  float acc[kTiles][kRows8][4] = {};
-  auto use = [&](const Block& b, int kb) {
-    uint32_t grid[kTiles];
-#pragma unroll
-    for (int i = 0; i < kTiles; ++i) grid[i] = kZeros ? b.scale[i] << 16 | b.zero[i] : b.scale[i] << 16;
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {                                              // 32 inputs, one group's
-      uint32_t xb[kRows8][kParts][4];
+        for (int c = kParts - 1; c >= 0; --c) {                                // the smallest parts first
+          const uint32_t (&x)[4] = xb[kBoth ? h : 0][r][c];
+          mma_bf16(sum[r], va[0], vb[0], va[1], vb[1], x[0], x[1]);
+          mma_bf16(sum[r], va[2], vb[2], va[3], vb[3], x[2], x[3]);
+        }
+    };
+    auto scaled = [&](int i, int h, const float (&sum)[kRows8][4]) {
+      const uint16_t* sc = reinterpret_cast<const uint16_t*>(at + R::kGridAt) + (i * R::kGroups + (kFine ? 2 * d + h : d >> a.group_shift)) * 16 + g;
+      const float s0 = bf16_float(sc[0]), s1 = bf16_float(sc[8]);
 #pragma unroll
       for (int r = 0; r < kRows8; ++r) {
-        if constexpr (kAhead) {
-          b.x[r][h].parts(xb[r]);
-        } else {
-          Chunk<T> c;
-          c.load(rows[r], kb * 64 + h * 32 + t * 8, a.k);
-          c.parts(xb[r]);
-        }
+        acc[i][r][0] = fmaf(s0, sum[r][0], acc[i][r][0]); acc[i][r][1] = fmaf(s0, sum[r][1], acc[i][r][1]);
+        acc[i][r][2] = fmaf(s1, sum[r][2], acc[i][r][2]); acc[i][r][3] = fmaf(s1, sum[r][3], acc[i][r][3]);
       }
+    };
+    if (kBoth) {
 #pragma unroll
-      for (int i = 0; i < kTiles; ++i) {
-        uint32_t q[2], va[4], vb[4];                                           // of the filters g and g + 8
+      for (int i = 0; i < kNt; ++i) {
+        const uint4 w = *reinterpret_cast<const uint4*>(mine + i * 512);
+        float sum[kRows8][4] = {};
+        half(i, 0, w, sum);
+        if (kFine) {
+          scaled(i, 0, sum);
 #pragma unroll
-        for (int f = 0; f < 2; ++f) q[f] = __shfl_sync(0xffffffffu, grid[i], (lane & 28) + (kFine ? 2 * h : 0) + f);
-        const uint32_t words[2] = {h ? b.codes[i].z : b.codes[i].x, h ? b.codes[i].w : b.codes[i].y};
-        spread_codes(words[0], kZeros ? kBias128 + (q[0] & 0xffu) * 0x00010001u : 0x43084308u, va);
-        spread_codes(words[1], kZeros ? kBias128 + (q[1] & 0xffu) * 0x00010001u : 0x43084308u, vb);
-        const float s0 = __uint_as_float(q[0] & 0xffff0000u), s1 = __uint_as_float(q[1] & 0xffff0000u);
+          for (int r = 0; r < kRows8; ++r) sum[r][0] = sum[r][1] = sum[r][2] = sum[r][3] = 0.f;
+        }
+        half(i, 1, w, sum);
+        scaled(i, 1, sum);
+      }
+    } else {
 #pragma unroll
-        for (int r = 0; r < kRows8; ++r) {
-          float sum[4] = {};
+      for (int h = 0; h < 2; ++h) {
 #pragma unroll
-          for (int c = kParts - 1; c >= 0; --c) {                              // the smallest parts first
-            mma_bf16(sum, va[0], vb[0], va[1], vb[1], xb[r][c][0], xb[r][c][1]);
-            mma_bf16(sum, va[2], vb[2], va[3], vb[3], xb[r][c][2], xb[r][c][3]);
-          }
-          acc[i][r][0] = fmaf(s0, sum[0], acc[i][r][0]); acc[i][r][1] = fmaf(s0, sum[1], acc[i][r][1]);
-          acc[i][r][2] = fmaf(s1, sum[2], acc[i][r][2]); acc[i][r][3] = fmaf(s1, sum[3], acc[i][r][3]);
+        for (int r = 0; r < kRows8; ++r) Operand<T>::read(x_at + (r * 2 + h) * kUnits * 512, xb[0][r]);
+#pragma unroll
+        for (int i = 0; i < kNt; ++i) {
+          const uint4 w = *reinterpret_cast<const uint4*>(mine + i * 512);
+          float sum[kRows8][4] = {};
+          half(i, h, w, sum);
+          scaled(i, h, sum);
         }
       }
     }
   };
 
-  const int step = 8 * int(ranks);
-  int kb = int(rank) * 8 + warp;
-  if (kb < a.k_blocks) {
-    Block now, next;
-    fetch(now, kb);
-    for (; kb + step < a.k_blocks; kb += step) {
-      fetch(next, kb + step);
-      use(now, kb);
-      now = next;
-    }
-    use(now, kb);
+#pragma unroll 1
+  for (int s = 0; s < R::kDepth - 1; ++s) fetch();
+  const unsigned char* at = ring;
+  int kb = first;
+#pragma unroll 1
+  for (int s = 0; s < n; ++s, kb += step) {
+    copies_wait<R::kDepth - 2>();
+    __syncwarp();                                    // every lane's copies of this stage are there, and nobody reads the last one any more
+    fetch();
+#pragma unroll
+    for (int d = 0; d < R::kDeep; ++d)
+      if (kb + d < a.k_blocks) use(at, d);
+    at = at + R::kStage == ring + R::kDepth * R::kStage ? ring : at + R::kStage;
   }
+  copies_wait<0>();
+}
+
+template <typename T, int kTiles, int kRows8, bool kFine, bool kZeros>        // kFine: groups of 32, two to a block
+__global__ void __launch_bounds__(kLinearThreads, 2)
+linear_w4_kernel(const LinearArgs a) {
+  typedef Ring<T, kTiles, kRows8, kFine> R;
+  constexpr int kCols = kRows8 * 8, kOut = kTiles * 16 * kCols;
+  extern __shared__ __align__(128) unsigned char smem_raw[];
+  float* part = reinterpret_cast<float*>(smem_raw);                           // [8][kOut], where the rings were
+  pdl_entry();
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+  const uint32_t ranks = cluster_size(), rank = cluster_ctarank();
+  // This CTA's tiles: as many as the others', or one less.  CTAs n and n + n_sms run on one SM, as a rule, and share the tiles
+  // of n_sms th parts.
+  const int cta = int(blockIdx.x / ranks), n_ctas = int(gridDim.x / ranks);
+  const int tile0 = int((long long)cta * a.n_tiles / n_ctas), nt = int((long long)(cta + 1) * a.n_tiles / n_ctas) - tile0;
+  const long long row0 = (long long)blockIdx.y * kCols;
+  const int step = 8 * R::kDeep * int(ranks), first = (int(rank) * 8 + warp) * R::kDeep;
+  unsigned char* ring = smem_raw + warp * (R::kDepth * R::kStage);
+  float acc[kTiles][kRows8][4] = {};
+  if (nt == kTiles) linear_sums<T, kTiles, kTiles, kRows8, kFine, kZeros>(a, ring, tile0, row0, first, step, lane, acc);
+  else if constexpr (kTiles > 1) linear_sums<T, kTiles, kTiles - 1, kRows8, kFine, kZeros>(a, ring, tile0, row0, first, step, lane, acc);
+  __syncthreads();
 
   // the warps' sums, [filter][row of x]
 #pragma unroll
   for (int i = 0; i < kTiles; ++i)
 #pragma unroll
     for (int r = 0; r < kRows8; ++r) {
-      float* at = part[warp] + (i * 16 + g) * kCols + r * 8 + 2 * t;
+      float* at = part + warp * kOut + (i * 16 + g) * kCols + r * 8 + 2 * t;
       *reinterpret_cast<float2*>(at) = make_float2(acc[i][r][0], acc[i][r][1]);
       *reinterpret_cast<float2*>(at + 8 * kCols) = make_float2(acc[i][r][2], acc[i][r][3]);
     }
   __syncthreads();
   if (ranks > 1) {
     for (int o = threadIdx.x; o < kOut; o += kLinearThreads) {
-      float s = part[0][o];
+      float s = part[o];
 #pragma unroll
-      for (int w = 1; w < 8; ++w) s += part[w][o];
-      part[0][o] = s;
+      for (int w = 1; w < 8; ++w) s += part[w * kOut + o];
+      part[o] = s;
     }
     cluster_sync_all();
   }
   T* y = static_cast<T*>(a.y);
   // filters fastest, so that neighbouring threads write neighbouring values of y
-  for (int n = threadIdx.x + int(rank) * kLinearThreads; n < kOut; n += kLinearThreads * int(ranks)) {
-    const int f = n % (kTiles * 16), r = n / (kTiles * 16), o = f * kCols + r;
+  for (int v = threadIdx.x + int(rank) * kLinearThreads; v < kOut; v += kLinearThreads * int(ranks)) {
+    const int f = v % (kTiles * 16), r = v / (kTiles * 16), o = f * kCols + r;
     float s;
     if (ranks > 1) {
       s = 0.f;
-      for (uint32_t p = 0; p < ranks; ++p) s += ld_cluster_f32(mapa_shared(smem_u32(&part[0][o]), p));
+      for (uint32_t p = 0; p < ranks; ++p) s += ld_cluster_f32(mapa_shared(smem_u32(part + o), p));
     } else {
-      s = part[0][o];
+      s = part[o];
 #pragma unroll
-      for (int w = 1; w < 8; ++w) s += part[w][o];
+      for (int w = 1; w < 8; ++w) s += part[w * kOut + o];
     }
     const int i = tile0 * 16 + f;
-    if (i < a.m && row0 + r < a.rows) {
+    if (f < nt * 16 && i < a.m && row0 + r < a.rows) {
+      s *= 64.f;
       if (a.bias) s += __ldg(a.bias + i);
       store_value(y + (row0 + r) * a.y_pitch + i, a.relu ? relu_of(s) : s);
     }
@@ -369,38 +621,46 @@ int64_t rows_of(const rt3d_tensor* t) {
     if ((n *= e) >= (int64_t(1) << 31)) return -1;
   return n;
 }
-bool blocks_for(long long threads, int per_block, unsigned* blocks) {
-  const long long n = (threads + per_block - 1) / per_block;
-  *blocks = unsigned(n);
-  return n < (1ll << 31);
+// Every warp of the two kernels takes 128 inputs of a tile of filters.
+template <typename T, bool kQuantize, int kGroup32>
+rt3d_status launch_between(T* w, int64_t pitch, const rt3d_w4* q, cudaStream_t st) {
+  GridArgs a;
+  a.codes = reinterpret_cast<uint4*>(q->codes);
+  a.scales = q->scales; a.zeros = q->zeros; a.pitch = pitch;
+  a.m = q->m; a.k = q->k; a.n_groups = ceil_div(q->k, q->group); a.k_blocks = ceil_div(q->k, 64);
+  a.chunks = ceil_div(q->k, 128); a.total = a.chunks * ceil_div(q->m, 16);
+  const bool vec = (reinterpret_cast<uintptr_t>(w) | uintptr_t(pitch) * sizeof(T)) % 16 == 0;
+  LaunchSetup ls(dim3(unsigned((a.total + 7) / 8)), dim3(256), 0, st);                  // 8 warps a block: total < 2^31
+  if constexpr (kQuantize)
+    return launched(vec ? cudaLaunchKernelEx(&ls.cfg, w4_quantize_kernel<T, kGroup32, true>, (const T*)w, a)
+                        : cudaLaunchKernelEx(&ls.cfg, w4_quantize_kernel<T, kGroup32, false>, (const T*)w, a));
+  else
+    return launched(vec ? cudaLaunchKernelEx(&ls.cfg, w4_unpack_kernel<T, kGroup32, true>, w, a)
+                        : cudaLaunchKernelEx(&ls.cfg, w4_unpack_kernel<T, kGroup32, false>, w, a));
+}
+template <typename T, bool kQuantize>
+rt3d_status between(T* w, int64_t pitch, const rt3d_w4* q, void* stream) {
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  return q->group == 32 ? launch_between<T, kQuantize, 1>(w, pitch, q, st) : q->group == 64 ? launch_between<T, kQuantize, 2>(w, pitch, q, st)
+                                                                                            : launch_between<T, kQuantize, 4>(w, pitch, q, st);
 }
 
-template <typename T>
-rt3d_status quantize(const T* w, int64_t pitch, const rt3d_w4* q, cudaStream_t st) {
-  const int n_groups = ceil_div(q->k, q->group), k_blocks = ceil_div(q->k, 64);
-  const long long total = (long long)ceil_div(q->m, 16) * 16 * n_groups;
-  unsigned blocks;
-  if (!blocks_for(total, 128, &blocks)) return RT3D_ERR_UNSUPPORTED;
-  LaunchSetup ls(dim3(blocks), dim3(128), 0, st);
-  return launched(cudaLaunchKernelEx(&ls.cfg, w4_quantize_kernel<T>, w, (long long)pitch, q->m, q->k, q->group, n_groups, k_blocks,
-                                     reinterpret_cast<uint32_t*>(q->codes), q->scales, q->zeros, total));
-}
-template <typename T>
-rt3d_status unpack(const rt3d_w4* q, T* w, int64_t pitch, cudaStream_t st) {
-  const int n_groups = ceil_div(q->k, q->group), k_blocks = ceil_div(q->k, 64), words = ceil_div(q->k, 8);
-  const long long total = (long long)q->m * words;
-  unsigned blocks;
-  if (!blocks_for(total, 256, &blocks)) return RT3D_ERR_UNSUPPORTED;
-  LaunchSetup ls(dim3(blocks), dim3(256), 0, st);
-  return launched(cudaLaunchKernelEx(&ls.cfg, w4_unpack_kernel<T>, reinterpret_cast<const uint32_t*>(q->codes), q->scales, q->zeros, q->m,
-                                     q->k, q->group, n_groups, k_blocks, words, w, (long long)pitch, total));
-}
 template <typename T, int kTiles, int kRows8>
-rt3d_status launch_linear(const LinearArgs& a, bool fine, int ranks, cudaStream_t st) {
-  const dim3 grid(unsigned(ceil_div(a.n_tiles, kTiles) * ranks), unsigned(ceil_div(a.rows, kRows8 * 8)));
-  LaunchSetup ls(grid, dim3(kLinearThreads), 0, st, unsigned(ranks));
-  const auto kernel = a.zeros ? (fine ? linear_w4_kernel<T, kTiles, kRows8, true, true> : linear_w4_kernel<T, kTiles, kRows8, false, true>)
-                              : (fine ? linear_w4_kernel<T, kTiles, kRows8, true, false> : linear_w4_kernel<T, kTiles, kRows8, false, false>);
+rt3d_status launch_linear(const LinearArgs& a, bool fine, int ctas, int ranks, cudaStream_t st) {
+  const dim3 grid(unsigned(ctas * ranks), unsigned(ceil_div(a.rows, kRows8 * 8)));
+  const uint32_t smem = fine ? Ring<T, kTiles, kRows8, true>::kBytes : Ring<T, kTiles, kRows8, false>::kBytes;
+  LaunchSetup ls(grid, dim3(kLinearThreads), smem, st, unsigned(ranks));
+  void (*const kernels[2][2])(LinearArgs) = {{linear_w4_kernel<T, kTiles, kRows8, false, false>, linear_w4_kernel<T, kTiles, kRows8, false, true>},
+                                             {linear_w4_kernel<T, kTiles, kRows8, true, false>, linear_w4_kernel<T, kTiles, kRows8, true, true>}};
+  const auto kernel = kernels[fine][a.zeros != nullptr];
+  static std::atomic<bool> attr_done[kMaxDevices][2][2];        // the attribute is per device
+  const int dev = current_device_index();
+  if (dev < 0) return RT3D_ERR_CUDA;
+  std::atomic<bool>& done = attr_done[dev][fine][a.zeros != nullptr];
+  if (!done.load()) {
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem)) != cudaSuccess) return RT3D_ERR_CUDA;
+    done.store(true);
+  }
   return launched(cudaLaunchKernelEx(&ls.cfg, kernel, a));
 }
 template <typename T>
@@ -414,23 +674,29 @@ rt3d_status linear(const rt3d_tensor* x, const rt3d_w4* q, const float* bias, in
   // fp32 rows take three times the registers: 16 at a time at most, in two tiles
   constexpr bool kWide = sizeof(T) == 2;
   const int rows8 = rows <= 8 ? 1 : rows <= 16 || !kWide ? 2 : 4;
-  // Four tiles to a CTA (a quarter of the reads of x) where two CTAs an SM are left, inputs cut over a cluster or not;
-  // then inputs are cut until there are two CTAs an SM, or every warp has one block.
-  const int most_ranks = a.k_blocks >= 64 ? 8 : a.k_blocks >= 32 ? 4 : a.k_blocks >= 16 ? 2 : 1;
-  const long long row_sets = ceil_div64(rows, rows8 * 8);
-  int tiles = rows8 == 4 || (rows8 == 2 && !kWide) ? 2 : 4;
-  while (tiles > 1 && ceil_div(a.n_tiles, tiles) * row_sets * most_ranks < 2 * sms) tiles /= 2;
+  const int most = rows8 == 4 || (rows8 == 2 && !kWide) ? 2 : 4;
+  // One CTA an SM for up to two tiles each (4096 x 8192, one row: 7.3 us as 256 CTAs, 7.3 as 148; 16 rows: 12.0 and 10.7), two for
+  // more (16384 x 16384, 4 rows: 37.4 us as 342 CTAs of up to 3 tiles, 30.3 as 296 of up to 4).  With fewer tiles than that, the CTAs
+  // of a cluster share the inputs while every warp keeps eight blocks (16384 inputs of 1000 filters, one row: 7.9 us alone, 5.9
+  // shared by four; 4096 inputs of 487: 4.0 alone, 4.2 by two).
+  const int ctas = a.n_tiles <= sms ? a.n_tiles : a.n_tiles <= 2 * sms ? sms : 2 * sms * ceil_div(a.n_tiles, most * 2 * sms);
   int ranks = 1;
-  while (ranks < most_ranks && ceil_div(a.n_tiles, tiles) * row_sets * ranks < 2 * sms) ranks *= 2;
+  while (ranks < 8 && ctas < sms && ctas * ranks <= sms && rows <= rows8 * 8 && a.k_blocks >= 128 * ranks) ranks *= 2;
+  const int tiles = ceil_div(a.n_tiles, ctas);
+  if (tiles > most) return RT3D_ERR_UNSUPPORTED;
   const bool fine = q->group == 32;
-  if (rows8 == 1)
-    return tiles == 4 ? launch_linear<T, 4, 1>(a, fine, ranks, st) : tiles == 2 ? launch_linear<T, 2, 1>(a, fine, ranks, st)
-                                                                                : launch_linear<T, 1, 1>(a, fine, ranks, st);
-  if constexpr (kWide) {
-    if (rows8 == 4) return tiles == 2 ? launch_linear<T, 2, 4>(a, fine, ranks, st) : launch_linear<T, 1, 4>(a, fine, ranks, st);
-    if (tiles == 4) return launch_linear<T, 4, 2>(a, fine, ranks, st);
+  if (rows8 == 1) {
+    if (tiles == 1) return launch_linear<T, 1, 1>(a, fine, ctas, ranks, st);
+    if (tiles == 2) return launch_linear<T, 2, 1>(a, fine, ctas, ranks, st);
+    if (tiles == 3) return launch_linear<T, 3, 1>(a, fine, ctas, ranks, st);
+    return launch_linear<T, 4, 1>(a, fine, ctas, ranks, st);
   }
-  return tiles == 2 ? launch_linear<T, 2, 2>(a, fine, ranks, st) : launch_linear<T, 1, 2>(a, fine, ranks, st);
+  if constexpr (kWide) {
+    if (rows8 == 4) return tiles == 2 ? launch_linear<T, 2, 4>(a, fine, ctas, ranks, st) : launch_linear<T, 1, 4>(a, fine, ctas, ranks, st);
+    if (tiles == 3) return launch_linear<T, 3, 2>(a, fine, ctas, ranks, st);
+    if (tiles == 4) return launch_linear<T, 4, 2>(a, fine, ctas, ranks, st);
+  }
+  return tiles == 2 ? launch_linear<T, 2, 2>(a, fine, ctas, ranks, st) : launch_linear<T, 1, 2>(a, fine, ctas, ranks, st);
 }
 
 }  // namespace
@@ -454,16 +720,16 @@ rt3d_status rt3d_w4_quantize(const void* w, int dtype, int64_t pitch, const rt3d
   const rt3d_status s = check_matrix(w, dtype, pitch, q);
   if (s != RT3D_OK) return s;
   if (plan_only()) return RT3D_OK;
-  cudaStream_t st = static_cast<cudaStream_t>(stream);
-  return dtype == RT3D_BF16 ? quantize(static_cast<const __nv_bfloat16*>(w), pitch, q, st) : quantize(static_cast<const float*>(w), pitch, q, st);
+  return dtype == RT3D_BF16 ? between<__nv_bfloat16, true>(static_cast<__nv_bfloat16*>(const_cast<void*>(w)), pitch, q, stream)
+                            : between<float, true>(static_cast<float*>(const_cast<void*>(w)), pitch, q, stream);
 }
 
 rt3d_status rt3d_w4_unpack(const rt3d_w4* q, int dtype, void* w, int64_t pitch, void* stream) {
   const rt3d_status s = check_matrix(w, dtype, pitch, q);
   if (s != RT3D_OK) return s;
   if (plan_only()) return RT3D_OK;
-  cudaStream_t st = static_cast<cudaStream_t>(stream);
-  return dtype == RT3D_BF16 ? unpack(q, static_cast<__nv_bfloat16*>(w), pitch, st) : unpack(q, static_cast<float*>(w), pitch, st);
+  return dtype == RT3D_BF16 ? between<__nv_bfloat16, false>(static_cast<__nv_bfloat16*>(w), pitch, q, stream)
+                            : between<float, false>(static_cast<float*>(w), pitch, q, stream);
 }
 
 rt3d_status rt3d_linear_w4(const rt3d_tensor* x, const rt3d_w4* q, const float* bias, int relu, rt3d_tensor* y, void* stream) {

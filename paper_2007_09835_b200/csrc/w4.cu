@@ -46,12 +46,31 @@ __device__ __forceinline__ Grid grid_of(float low, float high, bool bad, bool ze
   q.zero = zeros && q.scale > 0.f ? fminf(fmaxf(rintf(__fdiv_rn(-low, q.scale)), 0.f), 15.f) : 8.f;
   return q;
 }
-// A quotient decides between two codes only next to a half: elsewhere the product with the rounded reciprocal, off by less than
-// 2^-19 of quotients up to 16, gives the same code.  (4096 x 8192 fp32, a division for every weight: 70 us; 30 this way.)
-__device__ __forceinline__ uint32_t code_of(float v, const Grid& q, float inv) {
-  float p = v * inv, r = rintf(p);
-  if (!(fabsf(fabsf(p - r) - 0.5f) >= 1e-5f)) r = rintf(__fdiv_rn(v, q.scale));      // a NaN (reciprocal out of range) too
-  return uint32_t(fminf(fmaxf(r + q.zero, 0.f), 15.f));
+// The codes of eight values as a word.  A quotient decides between two codes only next to a half: elsewhere the product with the
+// rounded reciprocal, off by less than 2^-19 of quotients up to 16, gives the same code, so eight values are divided only where one
+// of them is that near (or the reciprocal out of range: a NaN).  Whole numbers are made by adding 1.5 2^23 (ties to even, as the
+// rounding instruction, but on the pipe that has room) and read from the mantissa of 2^23 + code.
+__device__ __forceinline__ uint32_t pack_codes(const float (&v)[8], const Grid& q, float inv) {
+  constexpr float kWhole = 12582912.f;
+  uint32_t word = 0;
+  bool near = false;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const float p = v[e] * inv, r = __fadd_rn(__fadd_rn(p, kWhole), -kWhole);
+    near |= !(fabsf(p - r) < 0.49999f);
+    word += (__float_as_uint(fminf(fmaxf(r + q.zero, 0.f), 15.f) + 8388608.f) - 0x4B000000u) << shift_of(e);
+  }
+  if (near) {
+    word = 0;
+#pragma unroll 1
+    for (int e = 0; e < 8; ++e) {
+      float x = v[0];
+#pragma unroll
+      for (int i = 1; i < 8; ++i) x = e == i ? v[i] : x;
+      word |= uint32_t(fminf(fmaxf(rintf(__fdiv_rn(x, q.scale)) + q.zero, 0.f), 15.f)) << shift_of(e);
+    }
+  }
+  return word;
 }
 
 // Eight values of a row in memory, those from `n` on zero; kVec: on a 16-byte boundary.
@@ -78,14 +97,13 @@ __device__ __forceinline__ void load8(const __nv_bfloat16* p, int n, float (&v)[
   for (int e = 0; e < 8; ++e) v[e] = e < n ? __bfloat162float(p[e]) : 0.f;
 }
 template <bool kVec>
-__device__ __forceinline__ void store8(float* p, int n, const float (&v)[8]) {
-  if (kVec && n >= 8) {
-    reinterpret_cast<float4*>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
-    reinterpret_cast<float4*>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
+__device__ __forceinline__ void store4(float* p, int n, const float* v) {
+  if (kVec && n >= 4) {
+    *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
     return;
   }
 #pragma unroll
-  for (int e = 0; e < 8; ++e)
+  for (int e = 0; e < 4; ++e)
     if (e < n) p[e] = v[e];
 }
 template <bool kVec>
@@ -111,12 +129,14 @@ struct GridArgs {                    // of the two calls between 4-bit and plain
   uint8_t* zeros;
   long long pitch;
   int m, k, n_groups, k_blocks;
-  long long chunks, total;           // of 128 inputs in a row of tiles, and in all
+  long long chunks, total;           // what a warp takes, in a row of tiles and in all
 };
 
-// A warp takes 128 inputs of 16 filters, whole groups: lane 4 g + t has 8 inputs of the filters g and g + 8 in each of the four
-// 32s, which are the words that it packs; four lanes make a group's extremes.  Read once, written in runs of 512 bytes.
+// A warp takes 64 inputs of 16 filters, 128 where a group has as many: lane 4 g + t has 8 inputs of the filters g and g + 8 in each of
+// the 32s, which are the words that it packs; four lanes make a group's extremes.  Read once, written in runs of 512 bytes.
 // kGroup32: 32s in a group.
+template <int kGroup32>
+constexpr int kWarpBlocks = kGroup32 == 4 ? 2 : 1;          // blocks of 64 inputs that a warp takes
 template <typename T, int kGroup32, bool kVec>
 __global__ void __launch_bounds__(256)
 w4_quantize_kernel(const T* __restrict__ w, const GridArgs a) {
@@ -125,22 +145,23 @@ w4_quantize_kernel(const T* __restrict__ w, const GridArgs a) {
   if (unit >= a.total) return;
   const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   const long long tile = unit / a.chunks;
-  const int k0 = int(unit - tile * a.chunks) * 128;
-  uint32_t words[2][4];              // filter, 32 inputs
+  constexpr int kHalves = 2 * kWarpBlocks<kGroup32>;
+  const int k0 = int(unit - tile * a.chunks) * (32 * kHalves);
+  uint32_t words[2][kHalves];        // filter, 32 inputs
 #pragma unroll
   for (int f = 0; f < 2; ++f) {
     const int i = int(tile) * 16 + g + 8 * f;
     const T* row = w + (long long)i * a.pitch;
-    float v[4][8], low[4], high[4];
-    bool bad[4];
+    float v[kHalves][8], low[kHalves], high[kHalves];
+    bool bad[kHalves];
     uint32_t filled = 0x88888888u;                   // the codes of values of zero
 #pragma unroll
-    for (int b = 0; b < 4; ++b) {
+    for (int b = 0; b < kHalves; ++b) {
       const int at = k0 + b * 32 + t * 8;
       load8<kVec>(row + at, i < a.m ? a.k - at : 0, v[b]);
     }
 #pragma unroll
-    for (int b = 0; b < 4; ++b) {
+    for (int b = 0; b < kHalves; ++b) {
       low[b] = high[b] = 0.f;
       bad[b] = false;
 #pragma unroll
@@ -156,7 +177,7 @@ w4_quantize_kernel(const T* __restrict__ w, const GridArgs a) {
       }
     }
 #pragma unroll
-    for (int b = 0; b < 4; b += kGroup32) {
+    for (int b = 0; b < kHalves; b += kGroup32) {
 #pragma unroll
       for (int c = 1; c < kGroup32; ++c) {
         low[b] = fminf(low[b], low[b + c]); high[b] = fmaxf(high[b], high[b + c]); bad[b] |= bad[b + c];
@@ -173,16 +194,13 @@ w4_quantize_kernel(const T* __restrict__ w, const GridArgs a) {
       if (group < a.n_groups) filled = uint32_t(q.zero) * 0x11111111u;
 #pragma unroll
       for (int c = 0; c < kGroup32; ++c) {
-        uint32_t word = 0;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) word |= code_of(v[b + c][e], q, inv) << shift_of(e);
-        words[f][b + c] = q.scale > 0.f ? word : filled;
+        words[f][b + c] = q.scale > 0.f ? pack_codes(v[b + c], q, inv) : filled;
       }
     }
   }
   uint4* dst = a.codes + (tile * a.k_blocks + k0 / 64) * 32 + lane;
 #pragma unroll
-  for (int b = 0; b < 2; ++b)
+  for (int b = 0; b < kHalves / 2; ++b)
     if (k0 / 64 + b < a.k_blocks) dst[b * 32] = make_uint4(words[0][2 * b], words[1][2 * b], words[0][2 * b + 1], words[1][2 * b + 1]);
 }
 
@@ -194,26 +212,44 @@ w4_unpack_kernel(T* __restrict__ w, const GridArgs a) {
   if (unit >= a.total) return;
   const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   const long long tile = unit / a.chunks;
-  const int k0 = int(unit - tile * a.chunks) * 128;
+  const int k0 = int(unit - tile * a.chunks) * (64 * kWarpBlocks<kGroup32>);
   const uint4* src = a.codes + (tile * a.k_blocks + k0 / 64) * 32 + lane;
 #pragma unroll
-  for (int b = 0; b < 2; ++b) {
+  for (int b = 0; b < kWarpBlocks<kGroup32>; ++b) {
     if (k0 / 64 + b >= a.k_blocks) return;
     const uint4 u = __ldg(src + b * 32);
     const uint32_t words[4] = {u.x, u.y, u.z, u.w};
+    // Two runs of 4 floats 16 apart, from the words of the lanes 4 g + t / 2 and 4 g + 2 + t / 2: four lanes' stores then fill
+    // 64 bytes of a row (with 8 in a row, 16 of every 32: 36 us for 4096 x 8192 instead of 26).  8 bf16 fill their sectors.
+    constexpr bool kTwoRuns = sizeof(T) == 4;
 #pragma unroll
     for (int f = 0; f < 2; ++f) {
       const int i = int(tile) * 16 + g + 8 * f;
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        const int at = k0 + b * 64 + h * 32 + t * 8;
+        uint32_t word[2] = {words[2 * h + f], 0u};
+        if (kTwoRuns) {
+          const uint32_t mine = word[0];
+#pragma unroll
+          for (int j = 0; j < 2; ++j) word[j] = __shfl_sync(0xffffffffu, mine, (lane & 28) + 2 * j + (t >> 1)) >> (8 * (t & 1));
+        }
+        const int at = k0 + b * 64 + h * 32;
         if (i >= a.m || at >= a.k) continue;
         const long long s_at = (tile * a.n_groups + at / (32 * kGroup32)) * 16 + g + 8 * f;
-        const float s = bf16_float(__ldg(a.scales + s_at)), z = a.zeros ? float(__ldg(a.zeros + s_at)) : 8.f;
+        const float s = bf16_float(__ldg(a.scales + s_at)), z = 8388608.f + (a.zeros ? float(__ldg(a.zeros + s_at)) : 8.f);
+        T* dst = w + (long long)i * a.pitch + at;
         float v[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = (float((words[2 * h + f] >> shift_of(e)) & 15u) - z) * s;
-        store8<kVec>(w + (long long)i * a.pitch + at, a.k - at, v);
+        for (int e = 0; e < 8; ++e) {                // 2^23 + code has the code in its mantissa
+          const uint32_t bits = kTwoRuns ? word[e >> 2] >> shift_of(e & 3) : word[0] >> shift_of(e);
+          v[e] = (__uint_as_float((bits & 15u) | 0x4B000000u) - z) * s;
+        }
+        if constexpr (kTwoRuns) {
+#pragma unroll
+          for (int j = 0; j < 2; ++j) store4<kVec>(dst + 16 * j + 4 * t, a.k - (at + 16 * j + 4 * t), v + 4 * j);
+        } else {
+          store8<kVec>(dst + 8 * t, a.k - (at + 8 * t), v);
+        }
       }
     }
   }
@@ -621,14 +657,13 @@ int64_t rows_of(const rt3d_tensor* t) {
     if ((n *= e) >= (int64_t(1) << 31)) return -1;
   return n;
 }
-// Every warp of the two kernels takes 128 inputs of a tile of filters.
 template <typename T, bool kQuantize, int kGroup32>
 rt3d_status launch_between(T* w, int64_t pitch, const rt3d_w4* q, cudaStream_t st) {
   GridArgs a;
   a.codes = reinterpret_cast<uint4*>(q->codes);
   a.scales = q->scales; a.zeros = q->zeros; a.pitch = pitch;
   a.m = q->m; a.k = q->k; a.n_groups = ceil_div(q->k, q->group); a.k_blocks = ceil_div(q->k, 64);
-  a.chunks = ceil_div(q->k, 128); a.total = a.chunks * ceil_div(q->m, 16);
+  a.chunks = ceil_div(q->k, 64 * kWarpBlocks<kGroup32>); a.total = a.chunks * ceil_div(q->m, 16);
   const bool vec = (reinterpret_cast<uintptr_t>(w) | uintptr_t(pitch) * sizeof(T)) % 16 == 0;
   LaunchSetup ls(dim3(unsigned((a.total + 7) / 8)), dim3(256), 0, st);                  // 8 warps a block: total < 2^31
   if constexpr (kQuantize)

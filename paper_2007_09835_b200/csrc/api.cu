@@ -1536,6 +1536,12 @@ rt3d_status current_device_info(DeviceInfo* info) {
   return s;
 }
 
+CUresult encode_tiled(CUtensorMap* map, CUtensorMapDataType type, cuuint32_t rank, void* data, const cuuint64_t* dims, const cuuint64_t* strides,
+                      const cuuint32_t* box, const cuuint32_t* steps, CUtensorMapSwizzle swizzle) {
+  return g_encode(map, type, rank, data, dims, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+}
+
 }  // namespace rt3d
 
 extern "C" {

@@ -1,22 +1,44 @@
 // Orthogonalised updates: Newton-Schulz products of a layer's gradient, and the optimiser step around them.
+//
+// With A = X X^T every step multiplies X by p(A) = a + b A + c A A, and the next A is p(A) A p(A): all of them polynomials in the
+// first A, which commute and are symmetric.  So a few steps are taken on the small n x n matrices (n the shorter side, l the longer)
+//     G = X X^T;   P_1 = p_1(G), G <- P_1 G P_1, P_2 = p_2(G), ..;   Q = .. P_2 P_1;   X <- Q X
+// which reads X twice for up to three steps instead of twice a step, and of a symmetric product only the tiles on and under the
+// diagonal are computed.  Squaring X loses the small singular values s where s^2 falls under the rounding of G; with 22 bits of G and
+// at most three steps to a run (which enlarge by at most 41 = 3.4445^3) nothing of weight is lost: against 64 bits 4e-7 to 5e-6 of |O| for
+// matrices whose singular values fall off as 1 to 1/i^2, where five steps in one run give NaN.
+// Values enter the tensor cores as fp16 parts, v = hi + lo (22 bits), products as hi hi + hi lo + lo hi with fp32 sums.  fp16's 11 bits
+// against bf16's 8: a bf16 gradient is its own hi part, and the X between two runs of rt3d_orthogonalize, whose result is bf16,
+// needs no lo part.  Matrices are held times a power of two (2^14, 2^10 for P and Q) so that lo parts stay normal numbers.
 #include <cuda_bf16.h>
+#include <cuda_fp16.h>
 #include <cuda_runtime.h>
 
+#include <atomic>
 #include <cmath>
 #include <cstdint>
+#include <cstring>
 
 #include "pdl.cuh"
 #include "rt3d.h"
 #include "rt3d_internal.h"
+#include "umma_common.cuh"
 
 namespace rt3d {
+
+CUresult encode_tiled(CUtensorMap* map, CUtensorMapDataType type, cuuint32_t rank, void* data, const cuuint64_t* dims, const cuuint64_t* strides,
+                      const cuuint32_t* box, const cuuint32_t* steps, CUtensorMapSwizzle swizzle);      // api.cu
+
 namespace {
 
 constexpr int kNormBlocks = 512;
+constexpr int kMostSteps = 16, kRuns = kMostSteps;
+constexpr float kXScale = 16384.f, kGScale = 16384.f, kPScale = 1024.f;        // what X, G and T, P and Q are held times
 
 __device__ __forceinline__ float value_of(const float* p) { return *p; }
 __device__ __forceinline__ float value_of(const __nv_bfloat16* p) { return __bfloat162float(*p); }
 
+// ------------------------------------------------------------------------------------------------ the matrix X of the first run
 // The matrix whose direction is wanted: a plain one, or the one of an optimiser step, whose momentum is brought up to date when
 // it is read first.
 template <typename T>
@@ -28,30 +50,67 @@ struct Source {
   float mu;
   int nesterov;
 };
-template <typename T, bool kFirst>
-__device__ __forceinline__ float source_value(const Source<T>& s, int i, int j, int k) {
-  if (!s.momentum) return value_of(s.g + (long long)i * s.pitch + j);
-  const long long at = (long long)i * k + j;
-  const bool keep = !s.mask || s.mask[at];
-  float v = s.momentum[at];
-  const float g = value_of(s.g + at);
-  if (kFirst) {
-    v = keep ? fmaf(s.mu, v, g) : 0.f;
-    s.momentum[at] = v;
+// Four neighbours of a row from column j on, those from `n` on zero.  kVec: all pointers allow wide accesses there.
+template <typename T, bool kVec>
+__device__ __forceinline__ void load4(const T* p, int n, float (&v)[4]) {
+  if (kVec) {
+    if constexpr (sizeof(T) == 4) {
+      const float4 a = *reinterpret_cast<const float4*>(p);
+      v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
+    } else {
+      const uint2 a = *reinterpret_cast<const uint2*>(p);
+      v[0] = __uint_as_float(a.x << 16); v[1] = __uint_as_float(a.x & 0xffff0000u);
+      v[2] = __uint_as_float(a.y << 16); v[3] = __uint_as_float(a.y & 0xffff0000u);
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = e < n ? value_of(p + e) : 0.f;
   }
-  return !keep ? 0.f : s.nesterov ? fmaf(s.mu, v, g) : v;
+}
+template <typename T, bool kFirst, bool kVec>
+__device__ __forceinline__ void source4(const Source<T>& s, int i, int j, int k, float (&v)[4]) {
+  const int n = k - j;
+  load4<T, kVec>(s.g + (long long)i * s.pitch + j, n, v);
+  if (!s.momentum) return;
+  const long long at = (long long)i * k + j;
+  uint32_t keep = 0x01010101u;
+  if (s.mask) {
+    if (kVec) keep = *reinterpret_cast<const uint32_t*>(s.mask + at);
+    else {
+      keep = 0;
+      for (int e = 0; e < 4 && e < n; ++e) keep |= uint32_t(s.mask[at + e]) << (8 * e);
+    }
+  }
+  float m[4];
+  load4<float, kVec>(s.momentum + at, n, m);
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const bool on = (keep >> (8 * e)) & 0xffu;
+    if (kFirst) m[e] = on ? fmaf(s.mu, m[e], v[e]) : 0.f;
+    v[e] = !on ? 0.f : s.nesterov ? fmaf(s.mu, m[e], v[e]) : m[e];
+  }
+  if (kFirst) {
+    if (kVec) *reinterpret_cast<float4*>(s.momentum + at) = make_float4(m[0], m[1], m[2], m[3]);
+    else
+      for (int e = 0; e < 4 && e < n; ++e) s.momentum[at + e] = m[e];
+  }
 }
 
 // Sums of squares of the blocks' shares, in 64 bits: neither overflow nor the order of a long sum matters.
-template <typename T>
+template <typename T, bool kVec>
 __global__ void __launch_bounds__(256)
 square_sums_kernel(Source<T> s, int m, int k, double* __restrict__ sums) {
   pdl_entry();
   __shared__ double part[8];
+  const unsigned quads = unsigned(k + 3) / 4;
+  const unsigned long long total = (unsigned long long)m * quads;
   double sum = 0.0;
-  for (long long idx = (long long)blockIdx.x * 256 + threadIdx.x; idx < (long long)m * k; idx += (long long)gridDim.x * 256) {
-    const float v = source_value<T, true>(s, int(idx / k), int(idx % k), k);
-    sum += double(v) * v;
+  for (unsigned long long idx = blockIdx.x * 256u + threadIdx.x; idx < total; idx += kNormBlocks * 256u) {
+    const int i = total >> 32 ? int(idx / quads) : int(unsigned(idx) / quads);
+    float v[4];
+    source4<T, true, kVec>(s, i, int(idx - (unsigned long long)i * quads) * 4, k, v);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) sum += double(v[e]) * v[e];
   }
   for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
   if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = sum;
@@ -62,73 +121,437 @@ square_sums_kernel(Source<T> s, int m, int k, double* __restrict__ sums) {
   }
 }
 
-// X = the source over its norm, transposed where there are more rows than columns.
-template <typename T>
-__global__ void __launch_bounds__(256)
-normalise_kernel(Source<T> s, int m, int k, const double* __restrict__ sums, double eps, float* __restrict__ x) {
-  pdl_entry();
-  double sum = 0.0;
-  for (int b = 0; b < kNormBlocks; ++b) sum += sums[b];
-  const double inv = 1.0 / (sqrt(sum) + eps);
-  for (long long idx = (long long)blockIdx.x * 256 + threadIdx.x; idx < (long long)m * k; idx += (long long)gridDim.x * 256) {
-    const int i = int(idx / k), j = int(idx % k);
-    x[m > k ? (long long)j * m + i : idx] = float(source_value<T, false>(s, i, j, k) * inv);
+__device__ __forceinline__ void split_half(float v, __half& hi, __half& lo) {
+  hi = __float2half_rn(v);
+  lo = __float2half_rn(v - __half2float(hi));
+}
+
+// The matrix of run r is F_r times what is held.  F_0 is the source over its norm and eps, of which a power of two is taken here,
+// which rounds nothing but what falls under fp16; where eps leaves less than 1/32 of a norm of one (a run enlarges by at most 50),
+// the next run's matrix is held times a power of two as well, so that the smallest gradients keep their bits too.
+// factors[r]: F_r^2, for G; factors[kRuns + r]: F_r / F_(r + 1), for X.
+__device__ void write_factors(double f, int runs, float* __restrict__ factors) {
+  for (int r = 0; r < runs; ++r) {
+    double next = 1.0;
+    if (r + 1 < runs && f < 1.0 / 32) next = exp2(ceil(log2(f * 64.0)));
+    factors[r] = float(f * f);
+    factors[kRuns + r] = float(f / next);
+    f = next;
   }
 }
 
-// C[i][j] = alpha sum_l A[i][l] B[l][j] + beta D[i][j]; strides of B given, the others row-major.
+// Blocks take 32 x 128 places; turned where there are more rows than columns, through shared memory.
+template <typename T, bool kVec>
 __global__ void __launch_bounds__(256)
-product_kernel(const float* __restrict__ a, long long lda, const float* __restrict__ b, long long b_row, long long b_col, int m, int n,
-               int k, float alpha, const float* __restrict__ d, float beta, float* __restrict__ c, long long ldc) {
+split_kernel(Source<T> s, int m, int k, const double* __restrict__ sums, double eps, int turned, __half* __restrict__ hi,
+             __half* __restrict__ lo, long long x_pitch, int runs, float* __restrict__ factors) {
   pdl_entry();
-  __shared__ float as[16][65], bs[16][65];
-  const int i0 = blockIdx.y * 64, j0 = blockIdx.x * 64, ti = threadIdx.x / 16, tj = threadIdx.x % 16;
-  float acc[4][4] = {};
-  for (int l0 = 0; l0 < k; l0 += 16) {
-    for (int q = threadIdx.x; q < 1024; q += 256) {
-      const int l = q % 16, r = q / 16;
-      as[l][r] = i0 + r < m && l0 + l < k ? a[(i0 + r) * lda + l0 + l] : 0.f;
-      const int bl = b_row == 1 ? l : q / 64, bj = b_row == 1 ? r : q % 64;
-      bs[bl][bj] = j0 + bj < n && l0 + bl < k ? b[(l0 + bl) * b_row + (j0 + bj) * b_col] : 0.f;
+  __shared__ double part[8];
+  __shared__ float tile[32][133];
+  double sum = sums[threadIdx.x] + sums[threadIdx.x + 256];
+  for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+  if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = sum;
+  __syncthreads();
+  sum = part[0];
+  for (int w = 1; w < 8; ++w) sum += part[w];
+  const double norm = sqrt(sum);
+  const bool number = norm > 0.0 && norm < 1e300;                // one that is none makes everything NaN
+  const double power = number ? exp2(floor(-log2(norm))) : 1.0;
+  if (blockIdx.x == 0 && threadIdx.x == 0)
+    write_factors(number ? 1.0 / ((norm + eps) * power) : norm == 0.0 ? 1.0 : __longlong_as_double(0x7fffffffffffffffll), runs, factors);
+  const double scale = power * kXScale;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int cols = (k + 127) / 128;
+  const int i0 = int(blockIdx.x / cols) * 32, j0 = int(blockIdx.x % cols) * 128;
+#pragma unroll
+  for (int p = 0; p < 4; ++p) {
+    const int r = p * 8 + warp, i = i0 + r, j = j0 + lane * 4;
+    if (i >= m || j >= k) continue;
+    float v[4];
+    source4<T, false, kVec>(s, i, j, k, v);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = float(v[e] * scale);
+    if (turned) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) tile[r][lane * 4 + e] = v[e];
+      continue;
     }
-    __syncthreads();
+    __half h[4], l[4];
 #pragma unroll
-    for (int l = 0; l < 16; ++l)
-#pragma unroll
-      for (int p = 0; p < 4; ++p)
-#pragma unroll
-        for (int q = 0; q < 4; ++q) acc[p][q] = fmaf(as[l][ti + 16 * p], bs[l][tj + 16 * q], acc[p][q]);
-    __syncthreads();
+    for (int e = 0; e < 4; ++e) split_half(v[e], h[e], l[e]);
+    __half *to = hi + i * x_pitch + j, *lo_to = lo + i * x_pitch + j;
+    if (j + 4 <= k) {                                            // the pitch is a multiple of 8
+      *reinterpret_cast<uint2*>(to) = *reinterpret_cast<const uint2*>(h);
+      if (lo) *reinterpret_cast<uint2*>(lo_to) = *reinterpret_cast<const uint2*>(l);
+    } else {
+      for (int e = 0; e < 4 && j + e < k; ++e) {
+        to[e] = h[e];
+        if (lo) lo_to[e] = l[e];
+      }
+    }
   }
-  for (int p = 0; p < 4; ++p)
+  if (!turned) return;
+  __syncthreads();
+  for (int c = warp; c < 128; c += 8) {
+    const int j = j0 + c, i = i0 + lane;
+    if (j >= k || i >= m) continue;
+    __half h, l;
+    split_half(tile[lane][c], h, l);
+    hi[j * x_pitch + i] = h;
+    if (lo) lo[j * x_pitch + i] = l;
+  }
+}
+
+// ------------------------------------------------------------------------------------------------------------- products
+constexpr int kTile = 128;                           // rows and columns of a tile
+constexpr uint32_t kOperand = kTile * 128;           // bytes of one operand of a stage: 128 x 64 fp16
+constexpr int kRing = 3;                             // stages of up to four operands
+constexpr int kProductThreads = 320;                 // producer, issuer, eight warps for the results
+constexpr uint32_t kProductSmem = kRing * 4 * kOperand + 1024 + sizeof(Barriers);
+
+enum { kOutParts = 0, kOutDirection = 1, kOutUpdate = 2 };
+
+// One product C = A B over chunks of 64: B^T's rows (K-major), or B's own (the last product, X).
+struct Problem {
+  CUtensorMap a[2], b[2];                            // hi and lo
+  int out;                                           // what becomes of C = alpha * factor * sum + diag I + beta D
+  float alpha, beta, diag;
+  const __half *d_hi, *d_lo;                         // D, or nullptr
+  __half *c_hi, *c_lo;                               // kOutParts; c_lo may be nullptr
+  long long pitch;                                   // of C and D, or of `bf`
+};
+struct ProductArgs {
+  Problem p[2];
+  int n_problems;                                    // 2: of equal extents
+  int parts;                                         // 1: hi hi; 2: hi hi + lo hi; 3: and hi lo
+  int same;                                          // A and B are the same matrix: a tile on the diagonal loads it once
+  int b_rows;                                        // B's own rows
+  int chunks, splits;
+  int symmetric;                                     // tiles on and under the diagonal, mirrored
+  int tiles_m, tiles_n, n_tiles;
+  int rows, cols;                                    // what of C exists (kOutParts of small matrices: all of the tiles)
+  const float* factor;                               // nullptr: 1
+  // results outside
+  int turned;                                        // C is written as its transpose
+  __nv_bfloat16* bf;
+  float* w;
+  const uint8_t* mask;
+  float keep_share, step;
+  long long w_pitch;
+  int32_t* err;
+};
+
+// fp16 x fp16 -> fp32, M = 128, N = 128, A K-major; B K-major or its own rows.
+__device__ __forceinline__ uint32_t instr_desc_f16(bool b_rows) {
+  return (1u << 4) | (b_rows ? 1u << 16 : 0u) | (uint32_t(kTile >> 3) << 17) | (uint32_t(kTile >> 4) << 24);
+}
+// B's own rows: 64 columns (128 bytes, swizzled) by rows of the sum; 8 rows 1024 bytes apart, 64 columns 8192.
+__device__ __forceinline__ uint64_t smem_desc_rows(uint32_t addr) {
+  return uint64_t((addr & 0x3FFFFu) >> 4) | uint64_t(8192 >> 4) << 16 | uint64_t(1024 >> 4) << 32 | uint64_t(1) << 46 | uint64_t(2) << 61;
+}
+
+struct TileAt { int problem, i, j; };
+__device__ __forceinline__ TileAt tile_at(const ProductArgs& a, int item) {
+  TileAt t;
+  t.problem = item / a.n_tiles;
+  item -= t.problem * a.n_tiles;
+  if (a.symmetric) {
+    t.i = int((sqrtf(8.f * float(item) + 1.f) - 1.f) * 0.5f);
+    while (t.i * (t.i + 1) / 2 > item) --t.i;
+    while ((t.i + 1) * (t.i + 2) / 2 <= item) ++t.i;
+    t.j = item - t.i * (t.i + 1) / 2;
+  } else {
+    t.j = item / a.tiles_m;                          // rows of tiles fastest: neighbours share B
+    t.i = item - t.j * a.tiles_m;
+  }
+  return t;
+}
+
+// 16 columns from c0 on of this thread's row of a tile.
+__device__ __forceinline__ void finish16(const ProductArgs& a, const Problem& p, const TileAt& t, int row, int c0, float (&v)[16], float alpha) {
+  const int i = t.i * kTile + row, j = t.j * kTile + c0;
+#pragma unroll
+  for (int e = 0; e < 16; ++e) v[e] *= alpha;
+  if (p.out == kOutParts) {
+    if (a.symmetric) {                               // small matrices, whole tiles
+      if (p.d_hi) {
+        const long long at = i * p.pitch + j;
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+          const uint4 h = *reinterpret_cast<const uint4*>(p.d_hi + at + 8 * q), l = *reinterpret_cast<const uint4*>(p.d_lo + at + 8 * q);
+          const __half2 *hh = reinterpret_cast<const __half2*>(&h), *ll = reinterpret_cast<const __half2*>(&l);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float2 x = __half22float2(hh[e]), y = __half22float2(ll[e]);
+            v[8 * q + 2 * e] += p.beta * (x.x + y.x); v[8 * q + 2 * e + 1] += p.beta * (x.y + y.y);
+          }
+        }
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          if (i == j + e) v[e] += p.diag;
+      }
+    } else if (i >= a.rows) {
+      return;
+    }
+    __half h[16], l[16];
+#pragma unroll
+    for (int e = 0; e < 16; ++e) split_half(v[e], h[e], l[e]);
+    const long long at = i * p.pitch + j;
+#pragma unroll
+    for (int q = 0; q < 2; ++q)
+      if (j + 8 * q < a.cols) {                      // the pitch is a multiple of 8: what lies behind the last column is padding
+        *reinterpret_cast<uint4*>(p.c_hi + at + 8 * q) = reinterpret_cast<const uint4*>(h)[q];
+        if (p.c_lo) *reinterpret_cast<uint4*>(p.c_lo + at + 8 * q) = reinterpret_cast<const uint4*>(l)[q];
+      }
+    if (a.symmetric && t.i != t.j) {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        p.c_hi[(j + e) * p.pitch + i] = h[e];
+        p.c_lo[(j + e) * p.pitch + i] = l[e];
+      }
+    }
+    return;
+  }
+  if (i >= a.rows) return;
+  const int n = a.cols - j;
+  if (p.out == kOutDirection) {
+    if (a.turned) {
+#pragma unroll
+      for (int e = 0; e < 16; ++e)
+        if (e < n) a.bf[(j + e) * a.w_pitch + i] = __float2bfloat16_rn(v[e]);
+      return;
+    }
+    __nv_bfloat16* to = a.bf + i * a.w_pitch + j;
+    if (n >= 16 && (reinterpret_cast<uintptr_t>(to) & 15) == 0) {
+      uint32_t o[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const __nv_bfloat162 b = __floats2bfloat162_rn(v[2 * e], v[2 * e + 1]);
+        o[e] = *reinterpret_cast<const uint32_t*>(&b);
+      }
+      reinterpret_cast<uint4*>(to)[0] = make_uint4(o[0], o[1], o[2], o[3]);
+      reinterpret_cast<uint4*>(to)[1] = make_uint4(o[4], o[5], o[6], o[7]);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 16; ++e)
+        if (e < n) to[e] = __float2bfloat16_rn(v[e]);
+    }
+    return;
+  }
+  if (a.turned) {
+#pragma unroll
+    for (int e = 0; e < 16; ++e)
+      if (e < n) {
+        const long long at = (j + e) * a.w_pitch + i;
+        a.w[at] = !a.mask || a.mask[at] ? fmaf(-a.step, v[e], a.keep_share * a.w[at]) : 0.f;
+      }
+    return;
+  }
+  const long long at = i * a.w_pitch + j;
+  float* to = a.w + at;
+  if (n >= 16 && ((reinterpret_cast<uintptr_t>(to) | (a.mask ? reinterpret_cast<uintptr_t>(a.mask + at) : 0)) & 15) == 0) {
+    uint4 keep = make_uint4(0x01010101u, 0x01010101u, 0x01010101u, 0x01010101u);
+    if (a.mask) keep = *reinterpret_cast<const uint4*>(a.mask + at);
+    const uint32_t k4[4] = {keep.x, keep.y, keep.z, keep.w};
+#pragma unroll
     for (int q = 0; q < 4; ++q) {
-      const int i = i0 + ti + 16 * p, j = j0 + tj + 16 * q;
-      if (i < m && j < n) c[i * ldc + j] = alpha * acc[p][q] + (d ? beta * d[i * ldc + j] : 0.f);
+      float4 x = reinterpret_cast<const float4*>(to)[q];
+      x.x = k4[q] & 0xffu ? fmaf(-a.step, v[4 * q], a.keep_share * x.x) : 0.f;
+      x.y = k4[q] & 0xff00u ? fmaf(-a.step, v[4 * q + 1], a.keep_share * x.y) : 0.f;
+      x.z = k4[q] & 0xff0000u ? fmaf(-a.step, v[4 * q + 2], a.keep_share * x.z) : 0.f;
+      x.w = k4[q] & 0xff000000u ? fmaf(-a.step, v[4 * q + 3], a.keep_share * x.w) : 0.f;
+      reinterpret_cast<float4*>(to)[q] = x;
     }
-}
-
-__global__ void direction_out_kernel(const float* __restrict__ x, int m, int k, __nv_bfloat16* __restrict__ out, long long pitch) {
-  pdl_entry();
-  for (long long idx = (long long)blockIdx.x * 256 + threadIdx.x; idx < (long long)m * k; idx += (long long)gridDim.x * 256) {
-    const int i = int(idx / k), j = int(idx % k);
-    out[i * pitch + j] = __float2bfloat16_rn(x[m > k ? (long long)j * m + i : idx]);
-  }
-}
-__global__ void apply_kernel(const float* __restrict__ x, int m, int k, const uint8_t* __restrict__ mask, float keep_share, float step,
-                             float* __restrict__ w) {
-  pdl_entry();
-  for (long long idx = (long long)blockIdx.x * 256 + threadIdx.x; idx < (long long)m * k; idx += (long long)gridDim.x * 256) {
-    const int i = int(idx / k), j = int(idx % k);
-    const float o = x[m > k ? (long long)j * m + i : idx];
-    w[idx] = !mask || mask[idx] ? fmaf(-step, o, keep_share * w[idx]) : 0.f;
+  } else {
+#pragma unroll
+    for (int e = 0; e < 16; ++e)
+      if (e < n) to[e] = !a.mask || a.mask[at + e] ? fmaf(-a.step, v[e], a.keep_share * to[e]) : 0.f;
   }
 }
 
-constexpr int kMostSteps = 16;
+// Tiles of 128 x 128: TMA fills a ring of stages (64 of the sum; up to four operands of 16 KB), one thread issues the products of a
+// stage's parts, eight warps take results from the two accumulators.  One tile after another in a CTA; or, with splits, one tile
+// for the CTAs of a cluster, which share the sum and add their parts up through one another's shared memory, 128 / splits columns
+// each (the small matrices are one to ten tiles: cutting the sum is what fills the SMs, and results are shared out with it).
+__global__ void __launch_bounds__(kProductThreads, 1)
+product_kernel(const __grid_constant__ ProductArgs a) {
+  extern __shared__ unsigned char smem_raw[];
+  const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+  Barriers* bars = reinterpret_cast<Barriers*>(smem_raw + (base - smem_u32(smem_raw)) + kRing * 4 * kOperand);
+  const int warp = uniform(int(threadIdx.x >> 5)), lane = threadIdx.x & 31;
+  const int n_items = a.n_tiles * a.n_problems;
+  const int split = a.splits > 1 ? int(cluster_ctarank()) : 0;
+  const int first = a.splits > 1 ? int(blockIdx.x) / a.splits : int(blockIdx.x), step = a.splits > 1 ? n_items : int(gridDim.x);
+  const int c_first = a.chunks * split / a.splits, c_last = a.chunks * (split + 1) / a.splits;
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < kRing; ++s) { mbar_init(smem_u32(&bars->full[s]), 1); mbar_init(smem_u32(&bars->empty[s]), 1); }
+    for (int b = 0; b < 2; ++b) { mbar_init(smem_u32(&bars->tmem_full[b]), 1); mbar_init(smem_u32(&bars->tmem_empty[b]), 8); }
+    bars->abort_flag = 0;
+    bars->wait_limit = kWaitCycles;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    for (int p = 0; p < a.n_problems; ++p)
+      for (int q = 0; q < 2; ++q) { tma_prefetch_map(&a.p[p].a[q]); tma_prefetch_map(&a.p[p].b[q]); }
+  }
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&bars->tmem_base)), "r"(256u) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = uniform(uint32_t(bars->tmem_base));
+  pdl_launch();
+  pdl_wait();
+
+  if (warp == 0) {
+    // ------------------------------------------------------------------ loads
+    if (lane == 0) {
+      int stage = 0;
+      uint32_t phase = 0;
+      bool ok = true;
+      for (int item = first; item < n_items && ok; item += step) {
+        const TileAt t = tile_at(a, item);
+        const Problem& p = a.p[t.problem];
+        const int a_parts = a.parts >= 2 ? 2 : 1, b_parts = (a.same && t.i == t.j) ? 0 : a.parts == 3 ? 2 : 1;
+        for (int c = c_first; c < c_last; ++c) {
+          const uint32_t full = smem_u32(&bars->full[stage]), at = base + stage * 4 * kOperand;
+          if (!mbar_wait(smem_u32(&bars->empty[stage]), phase ^ 1u, bars, a.err, 1)) { ok = false; break; }
+          mbar_expect_tx(full, uint32_t(a_parts + b_parts) * kOperand);
+          for (int q = 0; q < a_parts; ++q) tma_load_2d(at + q * kOperand, &p.a[q], full, c * 64, t.i * kTile);
+          for (int q = 0; q < b_parts; ++q) {
+            const uint32_t to = at + (2 + q) * kOperand;
+            if (a.b_rows) {
+              tma_load_2d(to, &p.b[q], full, t.j * kTile, c * 64);
+              tma_load_2d(to + kOperand / 2, &p.b[q], full, t.j * kTile + 64, c * 64);
+            } else {
+              tma_load_2d(to, &p.b[q], full, c * 64, t.j * kTile);
+            }
+          }
+          if (++stage == kRing) { stage = 0; phase ^= 1u; }
+        }
+      }
+    }
+  } else if (warp == 1) {
+    // ------------------------------------------------------------------ products
+    const bool elected = elect_one();
+    const uint32_t idesc = instr_desc_f16(a.b_rows != 0);
+    const uint64_t b_step = a.b_rows ? (16 * 128) >> 4 : 32 >> 4;         // 16 of the sum
+    uint32_t n = 0, phase = 0;
+    int stage = 0;
+    bool ok = true;
+    for (int item = first; item < n_items && ok; item += step, ++n) {
+      const TileAt t = tile_at(a, item);
+      const bool one = a.same && t.i == t.j;
+      const uint32_t buf = n & 1u, d = tmem + buf * kTile;
+      if (!mbar_wait_warp(smem_u32(&bars->tmem_empty[buf]), ((n >> 1) & 1u) ^ 1u, bars, a.err, 2)) break;
+      tc_fence_after();
+      for (int c = c_first; c < c_last; ++c) {
+        if (!mbar_wait_warp(smem_u32(&bars->full[stage]), phase, bars, a.err, 3)) { ok = false; break; }
+        tc_fence_after();
+        const uint32_t at = base + stage * 4 * kOperand, b_at = one ? at : at + 2 * kOperand;
+        const uint64_t a_hi = smem_desc_sw128(at), a_lo = smem_desc_sw128(at + kOperand);
+        const uint64_t b_hi = a.b_rows ? smem_desc_rows(b_at) : smem_desc_sw128(b_at);
+        const uint64_t b_lo = a.b_rows ? smem_desc_rows(b_at + kOperand) : smem_desc_sw128(b_at + kOperand);
+        if (elected) {
+          if (a.parts >= 2)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) umma_bf16(d, a_lo + 2 * k, b_hi + b_step * k, idesc, c > c_first || k ? 1u : 0u);
+          if (a.parts == 3)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) umma_bf16(d, a_hi + 2 * k, b_lo + b_step * k, idesc, 1u);
+#pragma unroll
+          for (int k = 0; k < 4; ++k) umma_bf16(d, a_hi + 2 * k, b_hi + b_step * k, idesc, c > c_first || k || a.parts >= 2 ? 1u : 0u);
+          umma_commit(smem_u32(&bars->empty[stage]));
+        }
+        if (++stage == kRing) { stage = 0; phase ^= 1u; }
+      }
+      if (!ok) break;
+      if (elected) umma_commit(smem_u32(&bars->tmem_full[buf]));
+    }
+    __syncwarp();
+  } else {
+    // ------------------------------------------------------------------ results
+    const int quad = warp & 3, half = (warp - 2) >> 2, row = quad * 32 + lane;
+    const float factor = a.factor ? *a.factor : 1.f;
+    uint32_t n = 0;
+    for (int item = first; item < n_items; item += step, ++n) {
+      const TileAt t = tile_at(a, item);
+      const Problem& p = a.p[t.problem];
+      const uint32_t buf = n & 1u;
+      if (!mbar_wait(smem_u32(&bars->tmem_full[buf]), (n >> 1) & 1u, bars, a.err, 4)) break;
+      tc_fence_after();
+      const uint32_t at = tmem + (uint32_t(quad * 32) << 16) + buf * kTile;
+      if (a.splits > 1) {            // this CTA's only tile: its part goes where the stages were, which every product has read
+        store_partial_row(at, kTile, true, reinterpret_cast<float*>(smem_raw + (base - smem_u32(smem_raw))) + row * kPartRow, half * 32, 64);
+      } else {
+#pragma unroll 1
+        for (int c0 = half * 16; c0 < kTile; c0 += 32) {
+          uint32_t r[16];
+          __syncwarp();
+          tmem_ld16(at + c0, r);
+          float v[16];
+#pragma unroll
+          for (int e = 0; e < 16; ++e) v[e] = __uint_as_float(r[e]);
+          finish16(a, p, t, row, c0, v, p.alpha * factor);
+        }
+      }
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(smem_u32(&bars->tmem_empty[buf]));
+    }
+    if (a.splits > 1) {
+      __syncwarp();
+      cluster_sync_all();
+      if (!bars->abort_flag) {
+        const TileAt t = tile_at(a, first);
+        const int units = kTile / 16, u1 = units * (split + 1) / a.splits;
+#pragma unroll 1
+        for (int u = units * split / a.splits + half; u < u1; u += 2) {
+          const uint32_t local = base + uint32_t(u * 16 * 128 + row * kPartRow) * 4u;
+          float v[16] = {};
+#pragma unroll 2
+          for (int q = 0; q < a.splits; ++q) {
+            const uint32_t remote = mapa_shared(local, uint32_t(q));
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              float4 x;
+              asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
+                           : "=f"(x.x), "=f"(x.y), "=f"(x.z), "=f"(x.w) : "r"(remote + e * 2048u) : "memory");
+              v[4 * e] += x.x; v[4 * e + 1] += x.y; v[4 * e + 2] += x.z; v[4 * e + 3] += x.w;
+            }
+          }
+          finish16(a, a.p[t.problem], t, row, u * 16, v, a.p[t.problem].alpha * factor);
+        }
+      }
+    }
+  }
+  if (a.splits > 1) {
+    __syncwarp();
+    if (warp < 2) cluster_sync_all();
+    cluster_sync_all();                              // nobody leaves while its part is still being read
+  }
+  if (bars->abort_flag) {
+    // give copies and products still in flight time to land before TMEM goes away
+    const long long t0 = clock64();
+    while (clock64() - t0 < 2000000ll) { }
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 1) {
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(256u) : "memory");
+  }
+}
+
+// ----------------------------------------------------------------------------------------------------------------- host
+constexpr double kMostOfRun = 50.0;                  // a run's P and Q, held times 2^10, stay in fp16
 struct Plan {
   int steps;
   double eps;
   float abc[kMostSteps][3];
+  double most[kMostSteps];                           // largest |p| of a step
 };
 
 // Largest |q(s)| over [0, top] of q = s (a + b s^2 + c s^4), and of p = a + b s^2 + c s^4: at the ends or where a derivative is zero.
@@ -166,30 +589,44 @@ rt3d_status make_plan(const rt3d_ortho_params* p, Plan* plan) {
     }
     double most_p;
     bounds_of(plan->abc[i][0], plan->abc[i][1], plan->abc[i][2], top, &top, &most_p);
-    if (!(top <= 1.9) || !(most_p <= 50.0)) return RT3D_ERR_UNSUPPORTED;
+    if (!(top <= 1.9) || !(most_p <= kMostOfRun)) return RT3D_ERR_UNSUPPORTED;
+    plan->most[i] = most_p;
   }
   return RT3D_OK;
 }
 
+
+struct Matrix {                                      // hi and lo parts, row-major
+  __half *hi, *lo;
+  int rows, cols;
+  long long pitch;
+};
 struct Workspace {
   double* sums;
-  float *x, *y, *gram, *poly;
+  float* factors;
+  Matrix x[2], g[2], p[2], t, q[2];
 };
-int64_t workspace_of(int m, int k, char* base, Workspace* ws) {
+int64_t workspace_of(int m, int k, char* base, Workspace* out) {
   int64_t at = 0;
   auto take = [&](int64_t bytes) {
     char* p = base + at;
     at += (bytes + 255) / 256 * 256;
     return p;
   };
-  const int64_t small = m < k ? m : k, size = int64_t(m) * k;
+  auto matrix = [&](int rows, int cols, int64_t pitch) {
+    Matrix x;
+    x.rows = rows; x.cols = cols; x.pitch = pitch;
+    x.hi = reinterpret_cast<__half*>(take(rows * pitch * 2));
+    x.lo = reinterpret_cast<__half*>(take(rows * pitch * 2));
+    return x;
+  };
+  const int n = m < k ? m : k, l = m < k ? k : m, side = int(ceil_div64(n, kTile)) * kTile;
   Workspace w;
   w.sums = reinterpret_cast<double*>(take(kNormBlocks * 8));
-  w.x = reinterpret_cast<float*>(take(size * 4));
-  w.y = reinterpret_cast<float*>(take(size * 4));
-  w.gram = reinterpret_cast<float*>(take(small * small * 4));
-  w.poly = reinterpret_cast<float*>(take(small * small * 4));
-  if (ws) *ws = w;
+  w.factors = reinterpret_cast<float*>(take(2 * kRuns * 4));
+  for (Matrix* x : {&w.x[0], &w.x[1]}) *x = matrix(n, l, ceil_div64(l, 8) * 8);
+  for (Matrix* x : {&w.g[0], &w.g[1], &w.p[0], &w.p[1], &w.t, &w.q[0], &w.q[1]}) *x = matrix(side, side, side);
+  if (out) *out = w;
   return at;
 }
 
@@ -199,29 +636,160 @@ rt3d_status launched(cudaError_t e) {
   return RT3D_OK;
 }
 
-rt3d_status product(const float* a, long long lda, const float* b, long long b_row, long long b_col, int m, int n, int k, float alpha,
-                    const float* d, float beta, float* c, long long ldc, cudaStream_t st) {
-  LaunchSetup ls(dim3(unsigned(ceil_div(n, 64)), unsigned(ceil_div(m, 64))), dim3(256), 0, st);
-  return launched(cudaLaunchKernelEx(&ls.cfg, product_kernel, a, lda, b, b_row, b_col, m, n, k, alpha, d, beta, c, ldc));
+struct Runner {
+  DeviceInfo dev;
+  cudaStream_t st;
+  int splits_of(int tiles, int chunks) const {
+    int s = 1;
+    while (s < 8 && tiles * s * 2 <= dev.sm_count && chunks >= 2 * s) s *= 2;
+    return s;
+  }
+  rt3d_status run(ProductArgs& a) const {
+    a.err = dev.err;
+    static std::atomic<bool> attr_done[kMaxDevices];
+    const int d = current_device_index();
+    if (d < 0) return RT3D_ERR_CUDA;
+    if (!attr_done[d].load()) {
+      if (cudaFuncSetAttribute(product_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(kProductSmem)) != cudaSuccess) return RT3D_ERR_CUDA;
+      attr_done[d].store(true);
+    }
+    const int items = a.n_tiles * a.n_problems;
+    a.splits = splits_of(items, a.chunks);
+    const int grid = a.splits > 1 ? items * a.splits : items < dev.sm_count ? items : dev.sm_count;
+    LaunchSetup ls(dim3(unsigned(grid)), dim3(kProductThreads), kProductSmem, st, unsigned(a.splits));
+    return launched(cudaLaunchKernelEx(&ls.cfg, product_kernel, a));
+  }
+  static bool map_of(CUtensorMap* map, const __half* p, const Matrix& x, int box_rows) {
+    const cuuint64_t dims[2] = {cuuint64_t(x.cols), cuuint64_t(x.rows)}, strides[1] = {cuuint64_t(x.pitch) * 2};
+    const cuuint32_t box[2] = {64, cuuint32_t(box_rows)}, estr[2] = {1, 1};
+    return encode_tiled(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, const_cast<__half*>(p), dims, strides, box, estr, CU_TENSOR_MAP_SWIZZLE_128B) == CUDA_SUCCESS;
+  }
+  static bool maps_of(CUtensorMap (&map)[2], const Matrix& x, int box_rows) { return map_of(&map[0], x.hi, x, box_rows) && map_of(&map[1], x.lo, x, box_rows); }
+
+  // G = X X^T (of one or two parts)
+  rt3d_status gram(const Matrix& x, int x_parts, const Matrix& g, const float* factor) const {
+    ProductArgs a;
+    std::memset(&a, 0, sizeof(a));
+    if (!maps_of(a.p[0].a, x, kTile) || !maps_of(a.p[0].b, x, kTile)) return RT3D_ERR_CUDA;
+    a.n_problems = 1; a.parts = x_parts == 2 ? 3 : 1; a.same = 1; a.symmetric = 1;
+    a.chunks = ceil_div(x.cols, 64);
+    a.tiles_m = a.tiles_n = g.rows / kTile; a.n_tiles = a.tiles_m * (a.tiles_m + 1) / 2;
+    a.rows = a.cols = g.rows;
+    a.factor = factor;
+    a.p[0].out = kOutParts; a.p[0].alpha = kGScale / (kXScale * kXScale); a.p[0].c_hi = g.hi; a.p[0].c_lo = g.lo; a.p[0].pitch = g.pitch;
+    return run(a);
+  }
+  // symmetric products of small matrices: problems made by `small`, one or two to a launch
+  bool small(Problem* p, const Matrix& l, const Matrix& r, const Matrix& c, float alpha, const Matrix* d = nullptr, float beta = 0.f, float diag = 0.f) const {
+    if (!maps_of(p->a, l, kTile) || !maps_of(p->b, r, kTile)) return false;
+    p->out = kOutParts; p->alpha = alpha; p->beta = beta; p->diag = diag;
+    p->d_hi = d ? d->hi : nullptr; p->d_lo = d ? d->lo : nullptr;
+    p->c_hi = c.hi; p->c_lo = c.lo; p->pitch = c.pitch;
+    return true;
+  }
+  rt3d_status small_products(ProductArgs& a, int n_problems, const Matrix& c) const {
+    a.n_problems = n_problems; a.parts = 3; a.symmetric = 1;
+    a.chunks = c.cols / 64;
+    a.tiles_m = a.tiles_n = c.rows / kTile; a.n_tiles = a.tiles_m * (a.tiles_m + 1) / 2;
+    a.rows = a.cols = c.rows;
+    return run(a);
+  }
+  // P = a + b G + c G G
+  rt3d_status polynomial(const Matrix& g, const Matrix& p, const float* abc) const {
+    ProductArgs a;
+    std::memset(&a, 0, sizeof(a));
+    if (!small(&a.p[0], g, g, p, abc[2] * kPScale / (kGScale * kGScale), &g, abc[1] * kPScale / kGScale, abc[0] * kPScale)) return RT3D_ERR_CUDA;
+    a.same = 1;
+    return small_products(a, 1, p);
+  }
+};
+
+// What becomes of the last product.
+struct Result {
+  int out, turned;
+  __nv_bfloat16* bf;
+  float* w;
+  const uint8_t* mask;
+  float keep_share, step;
+  long long pitch;
+};
+
+// Steps of the run that begins at step `done`, at most `most`.
+int run_steps(const Plan& plan, int done, int most) {
+  int steps = 1;
+  for (double p = plan.most[done]; steps < most && done + steps < plan.steps && (p *= plan.most[done + steps]) <= kMostOfRun;) ++steps;
+  return steps;
 }
 
-// X of the last step; *x is where it lies.
+// `first`: most steps of the first run; x_parts: parts of X in the first and in the others.
 template <typename T>
-rt3d_status direction(const Source<T>& src, int m, int k, const Plan& plan, const Workspace& ws, const float** x, cudaStream_t st) {
-  LaunchSetup ls(dim3(kNormBlocks), dim3(256), 0, st);
-  rt3d_status s = launched(cudaLaunchKernelEx(&ls.cfg, square_sums_kernel<T>, src, m, k, ws.sums));
+rt3d_status direction(const Source<T>& src, int m, int k, const Plan& plan, int first, const int (&x_parts)[2], const Workspace& ws, const Result& res,
+                      const DeviceInfo& dev, cudaStream_t st) {
+  const Runner r{dev, st};
+  const bool turned = m > k;
+  uintptr_t bits = reinterpret_cast<uintptr_t>(src.g) | uintptr_t(src.pitch) * sizeof(T);       // 4 values at a time
+  bool vec = k % 4 == 0 && bits % (4 * sizeof(T)) == 0;
+  if (src.momentum) vec = vec && reinterpret_cast<uintptr_t>(src.momentum) % 16 == 0 && reinterpret_cast<uintptr_t>(src.mask) % 4 == 0;
+  LaunchSetup l1(dim3(kNormBlocks), dim3(256), 0, st);
+  rt3d_status s = launched(vec ? cudaLaunchKernelEx(&l1.cfg, square_sums_kernel<T, true>, src, m, k, ws.sums)
+                               : cudaLaunchKernelEx(&l1.cfg, square_sums_kernel<T, false>, src, m, k, ws.sums));
   if (s != RT3D_OK) return s;
-  if ((s = launched(cudaLaunchKernelEx(&ls.cfg, normalise_kernel<T>, src, m, k, (const double*)ws.sums, plan.eps, ws.x))) != RT3D_OK) return s;
-  const int n = m < k ? m : k, l = m < k ? k : m;
-  float *cur = ws.x, *next = ws.y;
-  for (int i = 0; i < plan.steps; ++i) {
-    const float* abc = plan.abc[i];
-    if ((s = product(cur, l, cur, 1, l, n, n, l, 1.f, nullptr, 0.f, ws.gram, n, st)) != RT3D_OK) return s;
-    if ((s = product(ws.gram, n, ws.gram, n, 1, n, n, n, abc[2], ws.gram, abc[1], ws.poly, n, st)) != RT3D_OK) return s;
-    if ((s = product(ws.poly, n, cur, l, 1, n, l, n, 1.f, cur, abc[0], next, l, st)) != RT3D_OK) return s;
-    float* t = cur; cur = next; next = t;
+  const Matrix *x = &ws.x[0], *next = &ws.x[1];
+  __half* lo = x_parts[0] == 2 ? x->lo : nullptr;
+  int runs = 0;
+  for (int done = 0; done < plan.steps; ++runs) done += run_steps(plan, done, runs ? 3 : first);
+  const long long blocks = ceil_div64(m, 32) * ceil_div64(k, 128);
+  if (blocks >= (1ll << 31)) return RT3D_ERR_UNSUPPORTED;
+  LaunchSetup l2(dim3(unsigned(blocks)), dim3(256), 0, st);
+  s = launched(vec ? cudaLaunchKernelEx(&l2.cfg, split_kernel<T, true>, src, m, k, (const double*)ws.sums, plan.eps, int(turned), x->hi, lo, x->pitch, runs, ws.factors)
+                   : cudaLaunchKernelEx(&l2.cfg, split_kernel<T, false>, src, m, k, (const double*)ws.sums, plan.eps, int(turned), x->hi, lo, x->pitch, runs, ws.factors));
+  if (s != RT3D_OK) return s;
+  for (int done = 0, run = 0; done < plan.steps; ++run) {
+    const int parts = x_parts[run ? 1 : 0], steps = run_steps(plan, done, run ? 3 : first);
+    const Matrix *g = &ws.g[0], *g2 = &ws.g[1], *p = &ws.p[0], *p2 = &ws.p[1], *q = nullptr;
+    int q_next = 0;
+    if ((s = r.gram(*x, parts, *g, ws.factors + run)) != RT3D_OK) return s;
+    for (int i = 0; i < steps; ++i) {
+      if ((s = r.polynomial(*g, *p, plan.abc[done + i])) != RT3D_OK) return s;
+      ProductArgs a;
+      std::memset(&a, 0, sizeof(a));
+      int n = 0;
+      if (i + 1 < steps && !r.small(&a.p[n++], *p, *g, ws.t, kGScale / (kPScale * kGScale))) return RT3D_ERR_CUDA;       // T = P G
+      if (q) {                                                                                          // Q = P Q
+        if (!r.small(&a.p[n++], *p, *q, ws.q[q_next], 1.f / kPScale)) return RT3D_ERR_CUDA;
+        q = &ws.q[q_next];
+        q_next ^= 1;
+      }
+      if (n && (s = r.small_products(a, n, *p)) != RT3D_OK) return s;
+      if (i + 1 < steps) {                                                                              // G = T P
+        std::memset(&a, 0, sizeof(a));
+        if (!r.small(&a.p[0], ws.t, *p, *g2, 1.f / kPScale)) return RT3D_ERR_CUDA;
+        if ((s = r.small_products(a, 1, *g2)) != RT3D_OK) return s;
+        const Matrix* was = g; g = g2; g2 = was;
+      }
+      if (!q) { q = p; const Matrix* was = p; p = p2; p2 = was; }                                       // the first P is the first Q
+    }
+    done += steps;
+    const bool last = done == plan.steps;
+    ProductArgs a;
+    std::memset(&a, 0, sizeof(a));
+    Problem& c = a.p[0];
+    if (!Runner::maps_of(c.a, *q, kTile) || !Runner::maps_of(c.b, *x, 64)) return RT3D_ERR_CUDA;
+    a.n_problems = 1; a.parts = parts == 2 ? 3 : 2; a.b_rows = 1;
+    a.chunks = ceil_div(x->rows, 64);
+    a.tiles_m = ceil_div(x->rows, kTile); a.tiles_n = ceil_div(x->cols, kTile); a.n_tiles = a.tiles_m * a.tiles_n;
+    a.rows = x->rows; a.cols = x->cols;
+    a.factor = ws.factors + kRuns + run;
+    c.alpha = 1.f / kPScale;
+    if (last) {
+      c.out = res.out; c.alpha /= kXScale;
+      a.turned = res.turned; a.bf = res.bf; a.w = res.w; a.mask = res.mask; a.keep_share = res.keep_share; a.step = res.step; a.w_pitch = res.pitch;
+    } else {
+      c.out = kOutParts; c.c_hi = next->hi; c.c_lo = x_parts[1] == 2 ? next->lo : nullptr; c.pitch = next->pitch;
+    }
+    if ((s = r.run(a)) != RT3D_OK) return s;
+    const Matrix* was = x; x = next; next = was;
   }
-  *x = cur;
   return RT3D_OK;
 }
 
@@ -233,28 +801,25 @@ rt3d_status check_call(const void* g, int dtype, int m, int k, void* workspace, 
   return bytes < need ? RT3D_ERR_WORKSPACE : RT3D_OK;
 }
 
+
 template <typename T>
-rt3d_status orthogonalize(const T* g, int64_t pitch, int m, int k, const Plan& plan, __nv_bfloat16* out, int64_t out_pitch, char* base, cudaStream_t st) {
+rt3d_status orthogonalize(const T* g, int64_t pitch, int m, int k, const Plan& plan, __nv_bfloat16* out, int64_t out_pitch, char* base,
+                          const DeviceInfo& dev, cudaStream_t st) {
   Workspace ws;
   workspace_of(m, k, base, &ws);
-  const float* x = nullptr;
-  const rt3d_status s = direction(Source<T>{g, pitch, nullptr, nullptr, 0.f, 0}, m, k, plan, ws, &x, st);
-  if (s != RT3D_OK) return s;
-  LaunchSetup ls(dim3(kNormBlocks), dim3(256), 0, st);
-  return launched(cudaLaunchKernelEx(&ls.cfg, direction_out_kernel, x, m, k, out, (long long)out_pitch));
+  const Result res{kOutDirection, m > k, out, nullptr, nullptr, 0.f, 0.f, (long long)out_pitch};
+  const int parts[2] = {sizeof(T) == 2 ? 1 : 2, 1};
+  return direction(Source<T>{g, pitch, nullptr, nullptr, 0.f, 0}, m, k, plan, 3, parts, ws, res, dev, st);
 }
 
 template <typename T>
 rt3d_status update(float* w, float* momentum, const T* g, const uint8_t* mask, int m, int k, const rt3d_update_params& p, const Plan& plan,
-                   char* base, cudaStream_t st) {
+                   char* base, const DeviceInfo& dev, cudaStream_t st) {
   Workspace ws;
   workspace_of(m, k, base, &ws);
-  const float* x = nullptr;
-  const rt3d_status s = direction(Source<T>{g, k, momentum, mask, p.mu, p.nesterov}, m, k, plan, ws, &x, st);
-  if (s != RT3D_OK) return s;
-  LaunchSetup ls(dim3(kNormBlocks), dim3(256), 0, st);
-  return launched(cudaLaunchKernelEx(&ls.cfg, apply_kernel, x, m, k, mask, float(1.0 - double(p.lr) * p.weight_decay),
-                                     float(double(p.lr) * p.scale), w));
+  const Result res{kOutUpdate, m > k, nullptr, w, mask, float(1.0 - double(p.lr) * p.weight_decay), float(double(p.lr) * p.scale), k};
+  const int parts[2] = {2, 2};
+  return direction(Source<T>{g, k, momentum, mask, p.mu, p.nesterov}, m, k, plan, 2, parts, ws, res, dev, st);
 }
 
 }  // namespace
@@ -265,7 +830,7 @@ using namespace rt3d;
 extern "C" {
 
 int64_t rt3d_ortho_workspace(int m, int k) {
-  if (m < 1 || k < 1 || (m > 65535 && k > 65535)) return -1;
+  if (m < 1 || k < 1 || (m > 32768 && k > 32768) || m > (1 << 30) || k > (1 << 30)) return -1;
   return workspace_of(m, k, nullptr, nullptr);
 }
 
@@ -279,11 +844,14 @@ rt3d_status rt3d_orthogonalize(const void* g, int dtype, int64_t g_pitch, int m,
   const int64_t size = dtype == RT3D_BF16 ? 2 : 4;
   if (g0 < o0 + ((m - 1) * out_pitch + k) * 2 && o0 < g0 + ((m - 1) * g_pitch + k) * size) return RT3D_ERR_INVALID_ARG;
   if ((s = make_plan(p, &plan)) != RT3D_OK || plan_only()) return s;
+  DeviceInfo dev;
+  if ((s = current_device_info(&dev)) != RT3D_OK) return s;
+  if (dev.cc_major != 10) return RT3D_ERR_UNSUPPORTED;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   char* base = static_cast<char*>(workspace);
   __nv_bfloat16* o = static_cast<__nv_bfloat16*>(out);
-  return dtype == RT3D_BF16 ? orthogonalize(static_cast<const __nv_bfloat16*>(g), g_pitch, m, k, plan, o, out_pitch, base, st)
-                            : orthogonalize(static_cast<const float*>(g), g_pitch, m, k, plan, o, out_pitch, base, st);
+  return dtype == RT3D_BF16 ? orthogonalize(static_cast<const __nv_bfloat16*>(g), g_pitch, m, k, plan, o, out_pitch, base, dev, st)
+                            : orthogonalize(static_cast<const float*>(g), g_pitch, m, k, plan, o, out_pitch, base, dev, st);
 }
 
 rt3d_status rt3d_ortho_update(float* w, float* momentum, const void* g, int dtype, const uint8_t* mask, int m, int k,
@@ -301,10 +869,13 @@ rt3d_status rt3d_ortho_update(float* w, float* momentum, const void* g, int dtyp
     }
   if (!std::isfinite(p->lr) || !std::isfinite(p->mu) || !std::isfinite(p->weight_decay) || !std::isfinite(p->scale)) return RT3D_ERR_INVALID_ARG;
   if ((s = make_plan(&p->ortho, &plan)) != RT3D_OK || plan_only()) return s;
+  DeviceInfo dev;
+  if ((s = current_device_info(&dev)) != RT3D_OK) return s;
+  if (dev.cc_major != 10) return RT3D_ERR_UNSUPPORTED;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   char* base = static_cast<char*>(workspace);
-  return dtype == RT3D_BF16 ? update(w, momentum, static_cast<const __nv_bfloat16*>(g), mask, m, k, *p, plan, base, st)
-                            : update(w, momentum, static_cast<const float*>(g), mask, m, k, *p, plan, base, st);
+  return dtype == RT3D_BF16 ? update(w, momentum, static_cast<const __nv_bfloat16*>(g), mask, m, k, *p, plan, base, dev, st)
+                            : update(w, momentum, static_cast<const float*>(g), mask, m, k, *p, plan, base, dev, st);
 }
 
 }  // extern "C"

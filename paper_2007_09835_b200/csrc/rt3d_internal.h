@@ -235,6 +235,6 @@ void count_launches(int n);                               // for rt3d_launch_cou
 rt3d_status check_device_tensor(const rt3d_tensor* t);    // extents, dtype, pitch and alignment
 bool tensors_overlap(const rt3d_tensor* a, const rt3d_tensor* b);
 struct DeviceInfo { int sm_count, cc_major; int32_t* err; };      // err: the device's word for waits that gave up
-rt3d_status current_device_info(DeviceInfo* info);
+rt3d_status current_device_info(DeviceInfo* info);        // also makes encode_tiled usable
 
 }  // namespace rt3d

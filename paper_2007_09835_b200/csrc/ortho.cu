@@ -8,7 +8,7 @@
 // at most three steps to a run (which enlarge by at most 41 = 3.4445^3) nothing of weight is lost: against 64 bits 4e-7 to 5e-6 of |O| for
 // matrices whose singular values fall off as 1 to 1/i^2, where five steps in one run give NaN.
 // Values enter the tensor cores as fp16 parts, v = hi + lo (22 bits), products as hi hi + hi lo + lo hi with fp32 sums.  fp16's 11 bits
-// against bf16's 8: a bf16 gradient is its own hi part, and the X between two runs of rt3d_orthogonalize, whose result is bf16,
+// against bf16's 8: a bf16 gradient is its own hi part, and the X before the last steps of rt3d_orthogonalize, whose result is bf16,
 // needs no lo part.  Matrices are held times a power of two (2^14, 2^10 for P and Q) so that lo parts stay normal numbers.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -33,6 +33,7 @@ namespace {
 
 constexpr int kNormBlocks = 512;
 constexpr int kMostSteps = 16, kRuns = kMostSteps;
+constexpr int kFusedSide = 768, kFusedLength = 1024;
 constexpr float kXScale = 16384.f, kGScale = 16384.f, kPScale = 1024.f;        // what X, G and T, P and Q are held times
 
 __device__ __forceinline__ float value_of(const float* p) { return *p; }
@@ -144,7 +145,7 @@ __device__ void write_factors(double f, int runs, float* __restrict__ factors) {
 template <typename T, bool kVec>
 __global__ void __launch_bounds__(256)
 split_kernel(Source<T> s, int m, int k, const double* __restrict__ sums, double eps, int turned, __half* __restrict__ hi,
-             __half* __restrict__ lo, long long x_pitch, int runs, float* __restrict__ factors) {
+             __half* __restrict__ lo, long long x_pitch, int runs, float* __restrict__ factors, unsigned* __restrict__ arrived) {
   pdl_entry();
   __shared__ double part[8];
   __shared__ float tile[32][133];
@@ -154,6 +155,7 @@ split_kernel(Source<T> s, int m, int k, const double* __restrict__ sums, double 
   __syncthreads();
   sum = part[0];
   for (int w = 1; w < 8; ++w) sum += part[w];
+  if (blockIdx.x == 0 && threadIdx.x < kRuns) arrived[threadIdx.x] = 0;
   const double norm = sqrt(sum);
   const bool number = norm > 0.0 && norm < 1e300;                // one that is none makes everything NaN
   const double power = number ? exp2(floor(-log2(norm))) : 1.0;
@@ -203,34 +205,47 @@ split_kernel(Source<T> s, int m, int k, const double* __restrict__ sums, double 
 }
 
 // ------------------------------------------------------------------------------------------------------------- products
-constexpr int kTile = 128;                           // rows and columns of a tile
-constexpr uint32_t kOperand = kTile * 128;           // bytes of one operand of a stage: 128 x 64 fp16
-constexpr int kRing = 3;                             // stages of up to four operands
+constexpr int kTile = 128;                           // rows of a tile
+constexpr uint32_t kRowsBytes = kTile * 128;         // of 128 x 64 fp16
 constexpr int kProductThreads = 320;                 // producer, issuer, eight warps for the results
-constexpr uint32_t kProductSmem = kRing * 4 * kOperand + 1024 + sizeof(Barriers);
+constexpr uint32_t kRingBytes = 12 * kRowsBytes;
+constexpr uint32_t kProductSmem = kRingBytes + 1024 + sizeof(Barriers);
+constexpr int kMostProblems = 16;                    // of one launch
+
+// Tiles of 128 x kCols: a stage holds 64 of the sum of up to four operands (hi and lo of A and B).
+template <int kCols>
+struct Stage {
+  static constexpr uint32_t kColsBytes = kCols * 128, kBAt = 2 * kRowsBytes, kBytes = 2 * kRowsBytes + 2 * kColsBytes;
+  static constexpr int kRing = int(kRingBytes / kBytes);
+};
 
 enum { kOutParts = 0, kOutDirection = 1, kOutUpdate = 2 };
 
-// One product C = A B over chunks of 64: B^T's rows (K-major), or B's own (the last product, X).
+// One product C = A B: B^T's rows (K-major), or B's own (the last product of a run, X).
 struct Problem {
   CUtensorMap a[2], b[2];                            // hi and lo
   int out;                                           // what becomes of C = alpha * factor * sum + diag I + beta D
   float alpha, beta, diag;
+  const float* factor;                               // nullptr: 1
   const __half *d_hi, *d_lo;                         // D, or nullptr
   __half *c_hi, *c_lo;                               // kOutParts; c_lo may be nullptr
-  long long pitch;                                   // of C and D, or of `bf`
-};
-struct ProductArgs {
-  Problem p[2];
-  int n_problems;                                    // 2: of equal extents
+  long long pitch;                                   // of C and D
   int parts;                                         // 1: hi hi; 2: hi hi + lo hi; 3: and hi lo
   int same;                                          // A and B are the same matrix: a tile on the diagonal loads it once
   int b_rows;                                        // B's own rows
-  int chunks, splits;
   int symmetric;                                     // tiles on and under the diagonal, mirrored
-  int tiles_m, tiles_n, n_tiles;
-  int rows, cols;                                    // what of C exists (kOutParts of small matrices: all of the tiles)
-  const float* factor;                               // nullptr: 1
+  int chunks;
+  int tiles_m, n_tiles;
+  int rows, cols;                                    // what of C exists (symmetric: all of the tiles)
+};
+// Products of a launch: the problems [first[s], first[s + 1]) of a step run beside one another, every step after the one before.
+template <int kProblems>
+struct ProductArgs {
+  Problem p[kProblems];
+  int first[kProblems + 1];
+  int n_steps, splits;
+  int one_cluster;                                   // the grid is a cluster, which is what steps wait through
+  unsigned* arrived;                                 // else: CTAs that have reached the ends of steps, all together
   // results outside
   int turned;                                        // C is written as its transpose
   __nv_bfloat16* bf;
@@ -241,9 +256,10 @@ struct ProductArgs {
   int32_t* err;
 };
 
-// fp16 x fp16 -> fp32, M = 128, N = 128, A K-major; B K-major or its own rows.
+// fp16 x fp16 -> fp32, M = 128, A K-major; B K-major or its own rows.
+template <int kCols>
 __device__ __forceinline__ uint32_t instr_desc_f16(bool b_rows) {
-  return (1u << 4) | (b_rows ? 1u << 16 : 0u) | (uint32_t(kTile >> 3) << 17) | (uint32_t(kTile >> 4) << 24);
+  return (1u << 4) | (b_rows ? 1u << 16 : 0u) | (uint32_t(kCols >> 3) << 17) | (uint32_t(kTile >> 4) << 24);
 }
 // B's own rows: 64 columns (128 bytes, swizzled) by rows of the sum; 8 rows 1024 bytes apart, 64 columns 8192.
 __device__ __forceinline__ uint64_t smem_desc_rows(uint32_t addr) {
@@ -251,34 +267,40 @@ __device__ __forceinline__ uint64_t smem_desc_rows(uint32_t addr) {
 }
 
 struct TileAt { int problem, i, j; };
-__device__ __forceinline__ TileAt tile_at(const ProductArgs& a, int item) {
+template <int kCols, int kProblems>
+__device__ __forceinline__ TileAt tile_at(const ProductArgs<kProblems>& a, int s, int item) {
   TileAt t;
-  t.problem = item / a.n_tiles;
-  item -= t.problem * a.n_tiles;
-  if (a.symmetric) {
-    t.i = int((sqrtf(8.f * float(item) + 1.f) - 1.f) * 0.5f);
-    while (t.i * (t.i + 1) / 2 > item) --t.i;
-    while ((t.i + 1) * (t.i + 2) / 2 <= item) ++t.i;
-    t.j = item - t.i * (t.i + 1) / 2;
+  t.problem = a.first[s];
+  while (item >= a.p[t.problem].n_tiles) item -= a.p[t.problem++].n_tiles;
+  const Problem& p = a.p[t.problem];
+  if (p.symmetric) {                                 // tiles before row i: w i (i + 1) / 2 with w of kCols to a row of 128
+    constexpr int w = kTile / kCols;
+    t.i = int((sqrtf(8.f * float(item) / w + 1.f) - 1.f) * 0.5f);
+    while (w * t.i * (t.i + 1) / 2 > item) --t.i;
+    while (w * (t.i + 1) * (t.i + 2) / 2 <= item) ++t.i;
+    t.j = item - w * t.i * (t.i + 1) / 2;
   } else {
-    t.j = item / a.tiles_m;                          // rows of tiles fastest: neighbours share B
-    t.i = item - t.j * a.tiles_m;
+    t.j = item / p.tiles_m;                          // rows of tiles fastest: neighbours share B
+    t.i = item - t.j * p.tiles_m;
   }
   return t;
 }
+template <int kCols>
+__device__ __forceinline__ bool on_diagonal(const TileAt& t) { return (t.j + 1) * kCols > t.i * kTile; }
 
 // 16 columns from c0 on of this thread's row of a tile.
-__device__ __forceinline__ void finish16(const ProductArgs& a, const Problem& p, const TileAt& t, int row, int c0, float (&v)[16], float alpha) {
-  const int i = t.i * kTile + row, j = t.j * kTile + c0;
+template <int kCols, int kProblems>
+__device__ __forceinline__ void finish16(const ProductArgs<kProblems>& a, const Problem& p, const TileAt& t, int row, int c0, float (&v)[16], float alpha) {
+  const int i = t.i * kTile + row, j = t.j * kCols + c0;
 #pragma unroll
   for (int e = 0; e < 16; ++e) v[e] *= alpha;
   if (p.out == kOutParts) {
-    if (a.symmetric) {                               // small matrices, whole tiles
+    if (p.symmetric) {                               // small matrices, whole tiles
       if (p.d_hi) {
         const long long at = i * p.pitch + j;
 #pragma unroll
         for (int q = 0; q < 2; ++q) {
-          const uint4 h = *reinterpret_cast<const uint4*>(p.d_hi + at + 8 * q), l = *reinterpret_cast<const uint4*>(p.d_lo + at + 8 * q);
+          const uint4 h = __ldcg(reinterpret_cast<const uint4*>(p.d_hi + at + 8 * q)), l = __ldcg(reinterpret_cast<const uint4*>(p.d_lo + at + 8 * q));
           const __half2 *hh = reinterpret_cast<const __half2*>(&h), *ll = reinterpret_cast<const __half2*>(&l);
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
@@ -290,7 +312,7 @@ __device__ __forceinline__ void finish16(const ProductArgs& a, const Problem& p,
         for (int e = 0; e < 16; ++e)
           if (i == j + e) v[e] += p.diag;
       }
-    } else if (i >= a.rows) {
+    } else if (i >= p.rows) {
       return;
     }
     __half h[16], l[16];
@@ -299,11 +321,11 @@ __device__ __forceinline__ void finish16(const ProductArgs& a, const Problem& p,
     const long long at = i * p.pitch + j;
 #pragma unroll
     for (int q = 0; q < 2; ++q)
-      if (j + 8 * q < a.cols) {                      // the pitch is a multiple of 8: what lies behind the last column is padding
+      if (j + 8 * q < p.cols) {                      // the pitch is a multiple of 8: what lies behind the last column is padding
         *reinterpret_cast<uint4*>(p.c_hi + at + 8 * q) = reinterpret_cast<const uint4*>(h)[q];
         if (p.c_lo) *reinterpret_cast<uint4*>(p.c_lo + at + 8 * q) = reinterpret_cast<const uint4*>(l)[q];
       }
-    if (a.symmetric && t.i != t.j) {
+    if (p.symmetric && !on_diagonal<kCols>(t)) {
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
         p.c_hi[(j + e) * p.pitch + i] = h[e];
@@ -312,8 +334,8 @@ __device__ __forceinline__ void finish16(const ProductArgs& a, const Problem& p,
     }
     return;
   }
-  if (i >= a.rows) return;
-  const int n = a.cols - j;
+  if (i >= p.rows) return;
+  const int n = p.cols - j;
   if (p.out == kOutDirection) {
     if (a.turned) {
 #pragma unroll
@@ -369,33 +391,58 @@ __device__ __forceinline__ void finish16(const ProductArgs& a, const Problem& p,
   }
 }
 
-// Tiles of 128 x 128: TMA fills a ring of stages (64 of the sum; up to four operands of 16 KB), one thread issues the products of a
-// stage's parts, eight warps take results from the two accumulators.  One tile after another in a CTA; or, with splits, one tile
-// for the CTAs of a cluster, which share the sum and add their parts up through one another's shared memory, 128 / splits columns
-// each (the small matrices are one to ten tiles: cutting the sum is what fills the SMs, and results are shared out with it).
+// All CTAs of a cooperative grid have ended the step: `target` arrivals in all.  Bounded like every wait here.
+__device__ __forceinline__ void grid_barrier(unsigned* arrived, unsigned target, Barriers* bars, int32_t* err) {
+  __syncwarp();
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    __threadfence();
+    atomicAdd(arrived, 1u);
+    const long long start = clock64();
+    unsigned seen;
+    for (;;) {
+      asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(seen) : "l"(arrived) : "memory");
+      if (seen >= target) break;
+      if (clock64() - start > bars->wait_limit) {
+        bars->abort_flag = 1;
+        atomicCAS(err, 0, 5);
+        break;
+      }
+    }
+    __threadfence();
+  }
+  __syncthreads();
+}
+
+// TMA fills a ring of stages, one thread issues the products of a stage's parts, eight warps take results from the two accumulators:
+// one tile after another in a CTA.  With splits (one step, one tile to a cluster), the CTAs of a cluster share the sum and add
+// their parts up through one another's shared memory, 128 / splits columns each: the products X X^T have few tiles and long sums.
+// With several steps, the CTAs wait for one another between them, as one cluster or as a cooperative grid: a step on small matrices is
+// shorter than a launch.
+template <int kCols, int kProblems>
 __global__ void __launch_bounds__(kProductThreads, 1)
-product_kernel(const __grid_constant__ ProductArgs a) {
+product_kernel(const __grid_constant__ ProductArgs<kProblems> a) {
+  typedef Stage<kCols> S;
   extern __shared__ unsigned char smem_raw[];
   const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
-  Barriers* bars = reinterpret_cast<Barriers*>(smem_raw + (base - smem_u32(smem_raw)) + kRing * 4 * kOperand);
+  Barriers* bars = reinterpret_cast<Barriers*>(smem_raw + (base - smem_u32(smem_raw)) + kRingBytes);
   const int warp = uniform(int(threadIdx.x >> 5)), lane = threadIdx.x & 31;
-  const int n_items = a.n_tiles * a.n_problems;
   const int split = a.splits > 1 ? int(cluster_ctarank()) : 0;
-  const int first = a.splits > 1 ? int(blockIdx.x) / a.splits : int(blockIdx.x), step = a.splits > 1 ? n_items : int(gridDim.x);
-  const int c_first = a.chunks * split / a.splits, c_last = a.chunks * (split + 1) / a.splits;
+  const int cta = int(blockIdx.x) / a.splits, n_ctas = int(gridDim.x) / a.splits;
 
   if (threadIdx.x == 0) {
-    for (int s = 0; s < kRing; ++s) { mbar_init(smem_u32(&bars->full[s]), 1); mbar_init(smem_u32(&bars->empty[s]), 1); }
+    for (int s = 0; s < S::kRing; ++s) { mbar_init(smem_u32(&bars->full[s]), 1); mbar_init(smem_u32(&bars->empty[s]), 1); }
     for (int b = 0; b < 2; ++b) { mbar_init(smem_u32(&bars->tmem_full[b]), 1); mbar_init(smem_u32(&bars->tmem_empty[b]), 8); }
     bars->abort_flag = 0;
     bars->wait_limit = kWaitCycles;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-    for (int p = 0; p < a.n_problems; ++p)
+    for (int p = 0; p < a.first[1]; ++p)
       for (int q = 0; q < 2; ++q) { tma_prefetch_map(&a.p[p].a[q]); tma_prefetch_map(&a.p[p].b[q]); }
   }
   if (warp == 1) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&bars->tmem_base)), "r"(256u) : "memory");
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;"
+                 ::"r"(smem_u32(&bars->tmem_base)), "r"(uint32_t(2 * kCols)) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
   tc_fence_before();
@@ -405,132 +452,152 @@ product_kernel(const __grid_constant__ ProductArgs a) {
   pdl_launch();
   pdl_wait();
 
-  if (warp == 0) {
-    // ------------------------------------------------------------------ loads
-    if (lane == 0) {
-      int stage = 0;
-      uint32_t phase = 0;
+  int stage = 0;                                     // of this role: the ring and the accumulators go on from step to step
+  uint32_t phase = 0, n = 0;
+#pragma unroll 1
+  for (int s = 0; s < a.n_steps; ++s) {
+    int n_items = 0;
+    for (int p = a.first[s]; p < a.first[s + 1]; ++p) n_items += a.p[p].n_tiles;
+    if (warp == 0) {
+      // ---------------------------------------------------------------- loads
+      if (lane == 0) {
+        bool ok = true;
+        for (int item = cta; item < n_items && ok; item += n_ctas) {
+          const TileAt t = tile_at<kCols>(a, s, item);
+          const Problem& p = a.p[t.problem];
+          const bool one = kCols == kTile && p.same && t.i == t.j;
+          const int a_parts = p.parts >= 2 ? 2 : 1, b_parts = one ? 0 : p.parts == 3 ? 2 : 1;
+          const int c_last = p.chunks * (split + 1) / a.splits;
+          for (int c = p.chunks * split / a.splits; c < c_last; ++c) {
+            const uint32_t full = smem_u32(&bars->full[stage]), at = base + stage * S::kBytes;
+            if (!mbar_wait(smem_u32(&bars->empty[stage]), phase ^ 1u, bars, a.err, 1)) { ok = false; break; }
+            mbar_expect_tx(full, uint32_t(a_parts) * kRowsBytes + uint32_t(b_parts) * S::kColsBytes);
+            for (int q = 0; q < a_parts; ++q) tma_load_2d(at + q * kRowsBytes, &p.a[q], full, c * 64, t.i * kTile);
+            for (int q = 0; q < b_parts; ++q) {
+              const uint32_t to = at + S::kBAt + q * S::kColsBytes;
+              if (p.b_rows) {
+#pragma unroll
+                for (int h = 0; h < kCols / 64; ++h) tma_load_2d(to + h * 8192, &p.b[q], full, t.j * kCols + 64 * h, c * 64);
+              } else {
+                tma_load_2d(to, &p.b[q], full, c * 64, t.j * kCols);
+              }
+            }
+            if (++stage == S::kRing) { stage = 0; phase ^= 1u; }
+          }
+        }
+      }
+    } else if (warp == 1) {
+      // ---------------------------------------------------------------- products
+      const bool elected = elect_one();
       bool ok = true;
-      for (int item = first; item < n_items && ok; item += step) {
-        const TileAt t = tile_at(a, item);
+      for (int item = cta; item < n_items && ok; item += n_ctas, ++n) {
+        const TileAt t = tile_at<kCols>(a, s, item);
         const Problem& p = a.p[t.problem];
-        const int a_parts = a.parts >= 2 ? 2 : 1, b_parts = (a.same && t.i == t.j) ? 0 : a.parts == 3 ? 2 : 1;
-        for (int c = c_first; c < c_last; ++c) {
-          const uint32_t full = smem_u32(&bars->full[stage]), at = base + stage * 4 * kOperand;
-          if (!mbar_wait(smem_u32(&bars->empty[stage]), phase ^ 1u, bars, a.err, 1)) { ok = false; break; }
-          mbar_expect_tx(full, uint32_t(a_parts + b_parts) * kOperand);
-          for (int q = 0; q < a_parts; ++q) tma_load_2d(at + q * kOperand, &p.a[q], full, c * 64, t.i * kTile);
-          for (int q = 0; q < b_parts; ++q) {
-            const uint32_t to = at + (2 + q) * kOperand;
-            if (a.b_rows) {
-              tma_load_2d(to, &p.b[q], full, t.j * kTile, c * 64);
-              tma_load_2d(to + kOperand / 2, &p.b[q], full, t.j * kTile + 64, c * 64);
-            } else {
-              tma_load_2d(to, &p.b[q], full, c * 64, t.j * kTile);
-            }
-          }
-          if (++stage == kRing) { stage = 0; phase ^= 1u; }
-        }
-      }
-    }
-  } else if (warp == 1) {
-    // ------------------------------------------------------------------ products
-    const bool elected = elect_one();
-    const uint32_t idesc = instr_desc_f16(a.b_rows != 0);
-    const uint64_t b_step = a.b_rows ? (16 * 128) >> 4 : 32 >> 4;         // 16 of the sum
-    uint32_t n = 0, phase = 0;
-    int stage = 0;
-    bool ok = true;
-    for (int item = first; item < n_items && ok; item += step, ++n) {
-      const TileAt t = tile_at(a, item);
-      const bool one = a.same && t.i == t.j;
-      const uint32_t buf = n & 1u, d = tmem + buf * kTile;
-      if (!mbar_wait_warp(smem_u32(&bars->tmem_empty[buf]), ((n >> 1) & 1u) ^ 1u, bars, a.err, 2)) break;
-      tc_fence_after();
-      for (int c = c_first; c < c_last; ++c) {
-        if (!mbar_wait_warp(smem_u32(&bars->full[stage]), phase, bars, a.err, 3)) { ok = false; break; }
+        const bool one = kCols == kTile && p.same && t.i == t.j;
+        const uint32_t idesc = instr_desc_f16<kCols>(p.b_rows != 0);
+        const uint64_t b_step = p.b_rows ? (16 * 128) >> 4 : 32 >> 4;           // 16 of the sum
+        const uint32_t buf = n & 1u, d = tmem + buf * kCols;
+        if (!mbar_wait_warp(smem_u32(&bars->tmem_empty[buf]), ((n >> 1) & 1u) ^ 1u, bars, a.err, 2)) break;
         tc_fence_after();
-        const uint32_t at = base + stage * 4 * kOperand, b_at = one ? at : at + 2 * kOperand;
-        const uint64_t a_hi = smem_desc_sw128(at), a_lo = smem_desc_sw128(at + kOperand);
-        const uint64_t b_hi = a.b_rows ? smem_desc_rows(b_at) : smem_desc_sw128(b_at);
-        const uint64_t b_lo = a.b_rows ? smem_desc_rows(b_at + kOperand) : smem_desc_sw128(b_at + kOperand);
-        if (elected) {
-          if (a.parts >= 2)
+        const int c_first = p.chunks * split / a.splits, c_last = p.chunks * (split + 1) / a.splits;
+        for (int c = c_first; c < c_last; ++c) {
+          if (!mbar_wait_warp(smem_u32(&bars->full[stage]), phase, bars, a.err, 3)) { ok = false; break; }
+          tc_fence_after();
+          const uint32_t at = base + stage * S::kBytes, b_at = one ? at : at + S::kBAt, b_lo_at = one ? at + kRowsBytes : b_at + S::kColsBytes;
+          const uint64_t a_hi = smem_desc_sw128(at), a_lo = smem_desc_sw128(at + kRowsBytes);
+          const uint64_t b_hi = p.b_rows ? smem_desc_rows(b_at) : smem_desc_sw128(b_at);
+          const uint64_t b_lo = p.b_rows ? smem_desc_rows(b_lo_at) : smem_desc_sw128(b_lo_at);
+          if (elected) {
+            if (p.parts >= 2)
 #pragma unroll
-            for (int k = 0; k < 4; ++k) umma_bf16(d, a_lo + 2 * k, b_hi + b_step * k, idesc, c > c_first || k ? 1u : 0u);
-          if (a.parts == 3)
+              for (int k = 0; k < 4; ++k) umma_bf16(d, a_lo + 2 * k, b_hi + b_step * k, idesc, c > c_first || k ? 1u : 0u);
+            if (p.parts == 3)
 #pragma unroll
-            for (int k = 0; k < 4; ++k) umma_bf16(d, a_hi + 2 * k, b_lo + b_step * k, idesc, 1u);
+              for (int k = 0; k < 4; ++k) umma_bf16(d, a_hi + 2 * k, b_lo + b_step * k, idesc, 1u);
 #pragma unroll
-          for (int k = 0; k < 4; ++k) umma_bf16(d, a_hi + 2 * k, b_hi + b_step * k, idesc, c > c_first || k || a.parts >= 2 ? 1u : 0u);
-          umma_commit(smem_u32(&bars->empty[stage]));
+            for (int k = 0; k < 4; ++k) umma_bf16(d, a_hi + 2 * k, b_hi + b_step * k, idesc, c > c_first || k || p.parts >= 2 ? 1u : 0u);
+            umma_commit(smem_u32(&bars->empty[stage]));
+          }
+          if (++stage == S::kRing) { stage = 0; phase ^= 1u; }
         }
-        if (++stage == kRing) { stage = 0; phase ^= 1u; }
+        if (!ok) break;
+        if (elected) umma_commit(smem_u32(&bars->tmem_full[buf]));
       }
-      if (!ok) break;
-      if (elected) umma_commit(smem_u32(&bars->tmem_full[buf]));
-    }
-    __syncwarp();
-  } else {
-    // ------------------------------------------------------------------ results
-    const int quad = warp & 3, half = (warp - 2) >> 2, row = quad * 32 + lane;
-    const float factor = a.factor ? *a.factor : 1.f;
-    uint32_t n = 0;
-    for (int item = first; item < n_items; item += step, ++n) {
-      const TileAt t = tile_at(a, item);
-      const Problem& p = a.p[t.problem];
-      const uint32_t buf = n & 1u;
-      if (!mbar_wait(smem_u32(&bars->tmem_full[buf]), (n >> 1) & 1u, bars, a.err, 4)) break;
-      tc_fence_after();
-      const uint32_t at = tmem + (uint32_t(quad * 32) << 16) + buf * kTile;
-      if (a.splits > 1) {            // this CTA's only tile: its part goes where the stages were, which every product has read
-        store_partial_row(at, kTile, true, reinterpret_cast<float*>(smem_raw + (base - smem_u32(smem_raw))) + row * kPartRow, half * 32, 64);
-      } else {
+      __syncwarp();
+    } else {
+      // ---------------------------------------------------------------- results
+      const int quad = warp & 3, half = (warp - 2) >> 2, row = quad * 32 + lane;
+      for (int item = cta; item < n_items; item += n_ctas, ++n) {
+        const TileAt t = tile_at<kCols>(a, s, item);
+        const Problem& p = a.p[t.problem];
+        const float alpha = p.factor ? p.alpha * __ldcg(p.factor) : p.alpha;
+        const uint32_t buf = n & 1u;
+        if (!mbar_wait_warp(smem_u32(&bars->tmem_full[buf]), (n >> 1) & 1u, bars, a.err, 4)) break;
+        tc_fence_after();
+        const uint32_t at = tmem + (uint32_t(quad * 32) << 16) + buf * kCols;
+        if (a.splits > 1) {          // this CTA's only tile: its part goes where the stages were, which every product has read
+          store_partial_row(at, kCols, true, reinterpret_cast<float*>(smem_raw + (base - smem_u32(smem_raw))) + row * kPartRow, half * 32, 64);
+        } else {
 #pragma unroll 1
-        for (int c0 = half * 16; c0 < kTile; c0 += 32) {
-          uint32_t r[16];
-          __syncwarp();
-          tmem_ld16(at + c0, r);
-          float v[16];
+          for (int c0 = half * 16; c0 < kCols; c0 += 32) {
+            uint32_t r[16];
+            __syncwarp();
+            tmem_ld16(at + c0, r);
+            float v[16];
 #pragma unroll
-          for (int e = 0; e < 16; ++e) v[e] = __uint_as_float(r[e]);
-          finish16(a, p, t, row, c0, v, p.alpha * factor);
+            for (int e = 0; e < 16; ++e) v[e] = __uint_as_float(r[e]);
+            finish16<kCols>(a, p, t, row, c0, v, alpha);
+          }
         }
-      }
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(smem_u32(&bars->tmem_empty[buf]));
-    }
-    if (a.splits > 1) {
-      __syncwarp();
-      cluster_sync_all();
-      if (!bars->abort_flag) {
-        const TileAt t = tile_at(a, first);
-        const int units = kTile / 16, u1 = units * (split + 1) / a.splits;
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&bars->tmem_empty[buf]));
+        if (a.splits > 1) {
+          cluster_sync_all();
+          if (!bars->abort_flag) {
+            constexpr int units = kCols / 16;
+            const int u1 = units * (split + 1) / a.splits;
 #pragma unroll 1
-        for (int u = units * split / a.splits + half; u < u1; u += 2) {
-          const uint32_t local = base + uint32_t(u * 16 * 128 + row * kPartRow) * 4u;
-          float v[16] = {};
+            for (int u = units * split / a.splits + half; u < u1; u += 2) {
+              const uint32_t local = base + uint32_t(u * 16 * 128 + row * kPartRow) * 4u;
+              float v[16] = {};
 #pragma unroll 2
-          for (int q = 0; q < a.splits; ++q) {
-            const uint32_t remote = mapa_shared(local, uint32_t(q));
+              for (int q = 0; q < a.splits; ++q) {
+                const uint32_t remote = mapa_shared(local, uint32_t(q));
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              float4 x;
-              asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
-                           : "=f"(x.x), "=f"(x.y), "=f"(x.z), "=f"(x.w) : "r"(remote + e * 2048u) : "memory");
-              v[4 * e] += x.x; v[4 * e + 1] += x.y; v[4 * e + 2] += x.z; v[4 * e + 3] += x.w;
+                for (int e = 0; e < 4; ++e) {
+                  float4 x;
+                  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
+                               : "=f"(x.x), "=f"(x.y), "=f"(x.z), "=f"(x.w) : "r"(remote + e * 2048u) : "memory");
+                  v[4 * e] += x.x; v[4 * e + 1] += x.y; v[4 * e + 2] += x.z; v[4 * e + 3] += x.w;
+                }
+              }
+              finish16<kCols>(a, p, t, row, u * 16, v, alpha);
             }
           }
-          finish16(a, a.p[t.problem], t, row, u * 16, v, a.p[t.problem].alpha * factor);
         }
+      }
+    }
+    if (kProblems > 1 && s + 1 < a.n_steps) {        // what this step has written is what the next one's copies read
+      asm volatile("fence.proxy.async;" ::: "memory");
+      __threadfence();
+      if (a.one_cluster) {
+        __syncwarp();
+        cluster_sync_all();
+      } else {
+        grid_barrier(a.arrived, unsigned(s + 1) * gridDim.x, bars, a.err);
+      }
+      asm volatile("fence.proxy.async;" ::: "memory");
+      if (bars->abort_flag) {                        // this CTA's steps end here; the others' waits run out
+        if (!a.one_cluster) break;
       }
     }
   }
   if (a.splits > 1) {
+    // the results' warps have waited once, the others not; and nobody leaves while its part is still being read
     __syncwarp();
-    if (warp < 2) cluster_sync_all();
-    cluster_sync_all();                              // nobody leaves while its part is still being read
+    if (warp < 2 || n == 0) cluster_sync_all();
+    cluster_sync_all();
   }
   if (bars->abort_flag) {
     // give copies and products still in flight time to land before TMEM goes away
@@ -541,7 +608,7 @@ product_kernel(const __grid_constant__ ProductArgs a) {
   __syncthreads();
   if (warp == 1) {
     tc_fence_after();
-    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(256u) : "memory");
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(uint32_t(2 * kCols)) : "memory");
   }
 }
 
@@ -604,6 +671,7 @@ struct Matrix {                                      // hi and lo parts, row-maj
 struct Workspace {
   double* sums;
   float* factors;
+  unsigned* arrived;                                 // [kRuns], of the launches with several steps
   Matrix x[2], g[2], p[2], t, q[2];
 };
 int64_t workspace_of(int m, int k, char* base, Workspace* out) {
@@ -624,6 +692,7 @@ int64_t workspace_of(int m, int k, char* base, Workspace* out) {
   Workspace w;
   w.sums = reinterpret_cast<double*>(take(kNormBlocks * 8));
   w.factors = reinterpret_cast<float*>(take(2 * kRuns * 4));
+  w.arrived = reinterpret_cast<unsigned*>(take(kRuns * 4));
   for (Matrix* x : {&w.x[0], &w.x[1]}) *x = matrix(n, l, ceil_div64(l, 8) * 8);
   for (Matrix* x : {&w.g[0], &w.g[1], &w.p[0], &w.p[1], &w.t, &w.q[0], &w.q[1]}) *x = matrix(side, side, side);
   if (out) *out = w;
@@ -636,29 +705,11 @@ rt3d_status launched(cudaError_t e) {
   return RT3D_OK;
 }
 
+// Products as they are listed, and how they are launched: a step of its own each, or several steps in one launch.
 struct Runner {
   DeviceInfo dev;
   cudaStream_t st;
-  int splits_of(int tiles, int chunks) const {
-    int s = 1;
-    while (s < 8 && tiles * s * 2 <= dev.sm_count && chunks >= 2 * s) s *= 2;
-    return s;
-  }
-  rt3d_status run(ProductArgs& a) const {
-    a.err = dev.err;
-    static std::atomic<bool> attr_done[kMaxDevices];
-    const int d = current_device_index();
-    if (d < 0) return RT3D_ERR_CUDA;
-    if (!attr_done[d].load()) {
-      if (cudaFuncSetAttribute(product_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(kProductSmem)) != cudaSuccess) return RT3D_ERR_CUDA;
-      attr_done[d].store(true);
-    }
-    const int items = a.n_tiles * a.n_problems;
-    a.splits = splits_of(items, a.chunks);
-    const int grid = a.splits > 1 ? items * a.splits : items < dev.sm_count ? items : dev.sm_count;
-    LaunchSetup ls(dim3(unsigned(grid)), dim3(kProductThreads), kProductSmem, st, unsigned(a.splits));
-    return launched(cudaLaunchKernelEx(&ls.cfg, product_kernel, a));
-  }
+
   static bool map_of(CUtensorMap* map, const __half* p, const Matrix& x, int box_rows) {
     const cuuint64_t dims[2] = {cuuint64_t(x.cols), cuuint64_t(x.rows)}, strides[1] = {cuuint64_t(x.pitch) * 2};
     const cuuint32_t box[2] = {64, cuuint32_t(box_rows)}, estr[2] = {1, 1};
@@ -666,41 +717,108 @@ struct Runner {
   }
   static bool maps_of(CUtensorMap (&map)[2], const Matrix& x, int box_rows) { return map_of(&map[0], x.hi, x, box_rows) && map_of(&map[1], x.lo, x, box_rows); }
 
-  // G = X X^T (of one or two parts)
-  rt3d_status gram(const Matrix& x, int x_parts, const Matrix& g, const float* factor) const {
-    ProductArgs a;
-    std::memset(&a, 0, sizeof(a));
-    if (!maps_of(a.p[0].a, x, kTile) || !maps_of(a.p[0].b, x, kTile)) return RT3D_ERR_CUDA;
-    a.n_problems = 1; a.parts = x_parts == 2 ? 3 : 1; a.same = 1; a.symmetric = 1;
-    a.chunks = ceil_div(x.cols, 64);
-    a.tiles_m = a.tiles_n = g.rows / kTile; a.n_tiles = a.tiles_m * (a.tiles_m + 1) / 2;
-    a.rows = a.cols = g.rows;
-    a.factor = factor;
-    a.p[0].out = kOutParts; a.p[0].alpha = kGScale / (kXScale * kXScale); a.p[0].c_hi = g.hi; a.p[0].c_lo = g.lo; a.p[0].pitch = g.pitch;
-    return run(a);
+  // tiles of n x n on and under the diagonal: as wide as 128 rows need, the last row as wide as n
+  static int tiles_under(int n, int cols) {
+    const int rows = ceil_div(n, kTile), w = kTile / cols;
+    return w * (rows - 1) * rows / 2 + (cols == kTile ? rows : ceil_div(n, cols));
   }
-  // symmetric products of small matrices: problems made by `small`, one or two to a launch
-  bool small(Problem* p, const Matrix& l, const Matrix& r, const Matrix& c, float alpha, const Matrix* d = nullptr, float beta = 0.f, float diag = 0.f) const {
-    if (!maps_of(p->a, l, kTile) || !maps_of(p->b, r, kTile)) return false;
-    p->out = kOutParts; p->alpha = alpha; p->beta = beta; p->diag = diag;
-    p->d_hi = d ? d->hi : nullptr; p->d_lo = d ? d->lo : nullptr;
-    p->c_hi = c.hi; p->c_lo = c.lo; p->pitch = c.pitch;
+  // G = X X^T (of one or two parts)
+  static bool gram(Problem* p, const Matrix& x, int x_parts, const Matrix& g, const float* factor, int cols) {
+    if (!maps_of(p->a, x, kTile) || !maps_of(p->b, x, cols)) return false;
+    p->parts = x_parts == 2 ? 3 : 1; p->same = 1; p->symmetric = 1;
+    p->chunks = ceil_div(x.cols, 64);
+    p->n_tiles = tiles_under(x.rows, cols);
+    p->rows = p->cols = g.rows;
+    p->factor = factor;
+    p->out = kOutParts; p->alpha = kGScale / (kXScale * kXScale); p->c_hi = g.hi; p->c_lo = g.lo; p->pitch = g.pitch;
     return true;
   }
-  rt3d_status small_products(ProductArgs& a, int n_problems, const Matrix& c) const {
-    a.n_problems = n_problems; a.parts = 3; a.symmetric = 1;
-    a.chunks = c.cols / 64;
-    a.tiles_m = a.tiles_n = c.rows / kTile; a.n_tiles = a.tiles_m * (a.tiles_m + 1) / 2;
-    a.rows = a.cols = c.rows;
-    return run(a);
+  // C = alpha L R of small symmetric matrices of which n x n exist
+  static bool small(Problem* p, int n, const Matrix& l, const Matrix& r, const Matrix& c, float alpha, int cols) {
+    if (!maps_of(p->a, l, kTile) || !maps_of(p->b, r, cols)) return false;
+    p->parts = 3; p->symmetric = 1;
+    p->chunks = ceil_div(n, 64);
+    p->n_tiles = tiles_under(n, cols);
+    p->rows = p->cols = c.rows;
+    p->out = kOutParts; p->alpha = alpha; p->c_hi = c.hi; p->c_lo = c.lo; p->pitch = c.pitch;
+    return true;
   }
   // P = a + b G + c G G
-  rt3d_status polynomial(const Matrix& g, const Matrix& p, const float* abc) const {
-    ProductArgs a;
+  static bool polynomial(Problem* p, int n, const Matrix& g, const Matrix& c, const float* abc, int cols) {
+    if (!small(p, n, g, g, c, abc[2] * kPScale / (kGScale * kGScale), cols)) return false;
+    p->same = 1;
+    p->beta = abc[1] * kPScale / kGScale; p->diag = abc[0] * kPScale;
+    p->d_hi = g.hi; p->d_lo = g.lo;
+    return true;
+  }
+  // C = alpha Q X
+  static bool apply(Problem* p, const Matrix& q, const Matrix& x, int x_parts, const float* factor, int cols) {
+    if (!maps_of(p->a, q, kTile) || !maps_of(p->b, x, 64)) return false;
+    p->parts = x_parts == 2 ? 3 : 2; p->b_rows = 1;
+    p->chunks = ceil_div(x.rows, 64);
+    p->tiles_m = ceil_div(x.rows, kTile); p->n_tiles = p->tiles_m * ceil_div(x.cols, cols);
+    p->rows = x.rows; p->cols = x.cols;
+    p->factor = factor; p->alpha = 1.f / kPScale;
+    return true;
+  }
+
+  template <int kCols, int kProblems>
+  rt3d_status launch(ProductArgs<kProblems>& a, int grid, unsigned cluster, bool cooperative) const {
+    const auto kernel = product_kernel<kCols, kProblems>;
+    static std::atomic<bool> attr_done[kMaxDevices];
+    const int d = current_device_index();
+    if (d < 0) return RT3D_ERR_CUDA;
+    if (!attr_done[d].load()) {
+      if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(kProductSmem)) != cudaSuccess) return RT3D_ERR_CUDA;
+      attr_done[d].store(true);
+    }
+    a.err = dev.err;
+    LaunchSetup ls(dim3(unsigned(grid)), dim3(kProductThreads), kProductSmem, st, cluster);
+    if (cooperative) {
+      ls.attr[0].id = cudaLaunchAttributeCooperative;
+      ls.attr[0].val.cooperative = 1;
+      ls.cfg.numAttrs = 1;
+    }
+    return launched(cudaLaunchKernelEx(&ls.cfg, kernel, a));
+  }
+  // One step of tiles of 128 x 128, the sums cut where there are few.
+  rt3d_status run(ProductArgs<2>& a, int n_problems) const {
+    int items = 0;
+    for (int i = 0; i < n_problems; ++i) items += a.p[i].n_tiles;
+    a.first[0] = 0; a.first[1] = n_problems; a.n_steps = 1;
+    a.splits = 1;
+    while (a.splits < 8 && items * a.splits * 2 <= dev.sm_count && a.p[0].chunks >= 2 * a.splits) a.splits *= 2;
+    return launch<kTile>(a, a.splits > 1 ? items * a.splits : items < dev.sm_count ? items : dev.sm_count, unsigned(a.splits), false);
+  }
+};
+
+// Steps of one launch, tiles of 128 x 64.
+struct Fused {
+  const Runner& r;
+  ProductArgs<kMostProblems> a;
+  int n_problems = 0;
+  explicit Fused(const Runner& runner) : r(runner) { reset(); }
+  void reset() {
     std::memset(&a, 0, sizeof(a));
-    if (!small(&a.p[0], g, g, p, abc[2] * kPScale / (kGScale * kGScale), &g, abc[1] * kPScale / kGScale, abc[0] * kPScale)) return RT3D_ERR_CUDA;
-    a.same = 1;
-    return small_products(a, 1, p);
+    n_problems = 0;
+  }
+  Problem* add() { return &a.p[n_problems++]; }
+  void end_step() { a.first[++a.n_steps] = n_problems; }
+  // A cluster's wait takes 0.5 us, a grid's 1.5: eight CTAs where going round more often than a grid would costs less than that
+  // (a chunk of three products of 128 x 64: 700 clocks).
+  rt3d_status run(unsigned* arrived) {
+    int most = 1, extra = 0;
+    for (int s = 0; s < a.n_steps; ++s) {
+      int items = 0;
+      for (int p = a.first[s]; p < a.first[s + 1]; ++p) items += a.p[p].n_tiles;
+      most = items > most ? items : most;
+      extra += (ceil_div(items, 8) - ceil_div(items, r.dev.sm_count)) * a.p[a.first[s]].chunks;
+    }
+    a.splits = 1;
+    a.one_cluster = extra * 700 <= a.n_steps * 1900;
+    a.arrived = arrived;
+    const int grid = a.one_cluster ? (most < 8 ? most : 8) : most < r.dev.sm_count ? most : r.dev.sm_count;
+    return r.launch<64>(a, grid, a.one_cluster ? unsigned(grid) : 1u, !a.one_cluster && a.n_steps > 1);
   }
 };
 
@@ -721,12 +839,22 @@ int run_steps(const Plan& plan, int done, int most) {
   return steps;
 }
 
-// `first`: most steps of the first run; x_parts: parts of X in the first and in the others.
+// Parts of the X that the step `done` reads, for a result in bf16: what its rounding leaves in directions of small singular values is
+// enlarged by the steps left.  2^-12 of fp16 times 12 is 2^-8.4 where such directions are all of X, and they never are: with singular
+// values as 1 / i^2, 2.0e-3 of |O| in all, of which bf16's rounding is 1.7e-3 (enlarged by 41: 3.6e-3).
+int later_parts(const Plan& plan, int done) {
+  double left = 1.0;
+  for (int i = done; i < plan.steps; ++i) left *= plan.most[i] > 1.0 ? plan.most[i] : 1.0;
+  return left <= 12.0 ? 1 : 2;
+}
+
+// `first`: most steps of the first run; `exact`: two parts of every X; else one of the first where one holds it.
 template <typename T>
-rt3d_status direction(const Source<T>& src, int m, int k, const Plan& plan, int first, const int (&x_parts)[2], const Workspace& ws, const Result& res,
+rt3d_status direction(const Source<T>& src, int m, int k, const Plan& plan, int first, bool exact, const Workspace& ws, const Result& res,
                       const DeviceInfo& dev, cudaStream_t st) {
   const Runner r{dev, st};
   const bool turned = m > k;
+  const bool short_x = (turned ? k : m) <= kFusedSide && (turned ? m : k) <= kFusedLength;
   uintptr_t bits = reinterpret_cast<uintptr_t>(src.g) | uintptr_t(src.pitch) * sizeof(T);       // 4 values at a time
   bool vec = k % 4 == 0 && bits % (4 * sizeof(T)) == 0;
   if (src.momentum) vec = vec && reinterpret_cast<uintptr_t>(src.momentum) % 16 == 0 && reinterpret_cast<uintptr_t>(src.mask) % 4 == 0;
@@ -735,60 +863,103 @@ rt3d_status direction(const Source<T>& src, int m, int k, const Plan& plan, int 
                                : cudaLaunchKernelEx(&l1.cfg, square_sums_kernel<T, false>, src, m, k, ws.sums));
   if (s != RT3D_OK) return s;
   const Matrix *x = &ws.x[0], *next = &ws.x[1];
-  __half* lo = x_parts[0] == 2 ? x->lo : nullptr;
+  int parts = !exact && sizeof(T) == 2 ? 1 : 2;
+  __half* lo = parts == 2 ? x->lo : nullptr;
   int runs = 0;
-  for (int done = 0; done < plan.steps; ++runs) done += run_steps(plan, done, runs ? 3 : first);
+  for (int done = 0; done < plan.steps; ++runs) done += run_steps(plan, done, short_x ? 1 : runs ? 3 : first);
   const long long blocks = ceil_div64(m, 32) * ceil_div64(k, 128);
   if (blocks >= (1ll << 31)) return RT3D_ERR_UNSUPPORTED;
   LaunchSetup l2(dim3(unsigned(blocks)), dim3(256), 0, st);
-  s = launched(vec ? cudaLaunchKernelEx(&l2.cfg, split_kernel<T, true>, src, m, k, (const double*)ws.sums, plan.eps, int(turned), x->hi, lo, x->pitch, runs, ws.factors)
-                   : cudaLaunchKernelEx(&l2.cfg, split_kernel<T, false>, src, m, k, (const double*)ws.sums, plan.eps, int(turned), x->hi, lo, x->pitch, runs, ws.factors));
+  s = launched(vec ? cudaLaunchKernelEx(&l2.cfg, split_kernel<T, true>, src, m, k, (const double*)ws.sums, plan.eps, int(turned), x->hi, lo, x->pitch, runs, ws.factors, ws.arrived)
+                   : cudaLaunchKernelEx(&l2.cfg, split_kernel<T, false>, src, m, k, (const double*)ws.sums, plan.eps, int(turned), x->hi, lo, x->pitch, runs, ws.factors, ws.arrived));
   if (s != RT3D_OK) return s;
+  // The small matrices' products are steps of one launch up to kFusedSide; where X is short as well, everything is, with runs of one
+  // step, which need the fewest products in a row.
+  const int n = turned ? k : m, n_fused = n <= kFusedSide;
+  int launch_no = 0;
+  ProductArgs<2> one;
+  std::memset(&one, 0, sizeof(one));
+  Fused chain(r);
+  auto flush = [&]() -> rt3d_status {
+    if (!chain.a.n_steps) return RT3D_OK;
+    const rt3d_status e = chain.run(ws.arrived + launch_no++);
+    chain.reset();
+    return e;
+  };
+  const Matrix *cur = x, *other = next;
   for (int done = 0, run = 0; done < plan.steps; ++run) {
-    const int parts = x_parts[run ? 1 : 0], steps = run_steps(plan, done, run ? 3 : first);
+    const int steps = run_steps(plan, done, short_x ? 1 : run ? 3 : first);
     const Matrix *g = &ws.g[0], *g2 = &ws.g[1], *p = &ws.p[0], *p2 = &ws.p[1], *q = nullptr;
+    const int cols = n_fused ? 64 : kTile;
     int q_next = 0;
-    if ((s = r.gram(*x, parts, *g, ws.factors + run)) != RT3D_OK) return s;
+    if (short_x) {
+      if (chain.n_problems + 3 > kMostProblems && (s = flush()) != RT3D_OK) return s;
+      if (!Runner::gram(chain.add(), *cur, parts, *g, ws.factors + run, cols)) return RT3D_ERR_CUDA;
+      chain.end_step();
+    } else {
+      std::memset(&one, 0, sizeof(one));
+      if (!Runner::gram(&one.p[0], *cur, parts, *g, ws.factors + run, kTile)) return RT3D_ERR_CUDA;
+      if ((s = r.run(one, 1)) != RT3D_OK) return s;
+    }
+    // a step of one or two products
+    auto products = [&](auto&& first_product, auto&& second_product, int count) -> rt3d_status {
+      if (n_fused) {
+        if (!first_product(chain.add()) || (count == 2 && !second_product(chain.add()))) return RT3D_ERR_CUDA;
+        chain.end_step();
+        return RT3D_OK;
+      }
+      std::memset(&one, 0, sizeof(one));
+      if (!first_product(&one.p[0]) || (count == 2 && !second_product(&one.p[1]))) return RT3D_ERR_CUDA;
+      return r.run(one, count);
+    };
     for (int i = 0; i < steps; ++i) {
-      if ((s = r.polynomial(*g, *p, plan.abc[done + i])) != RT3D_OK) return s;
-      ProductArgs a;
-      std::memset(&a, 0, sizeof(a));
-      int n = 0;
-      if (i + 1 < steps && !r.small(&a.p[n++], *p, *g, ws.t, kGScale / (kPScale * kGScale))) return RT3D_ERR_CUDA;       // T = P G
-      if (q) {                                                                                          // Q = P Q
-        if (!r.small(&a.p[n++], *p, *q, ws.q[q_next], 1.f / kPScale)) return RT3D_ERR_CUDA;
+      const bool more = i + 1 < steps;
+      auto make_p = [&](Problem* to) { return Runner::polynomial(to, n, *g, *p, plan.abc[done + i], cols); };
+      auto make_t = [&](Problem* to) { return Runner::small(to, n, *p, *g, ws.t, kGScale / (kPScale * kGScale), cols); };           // T = P G
+      auto make_q = [&](Problem* to) { return Runner::small(to, n, *p, *q, ws.q[q_next], 1.f / kPScale, cols); };                   // Q = P Q
+      auto make_g = [&](Problem* to) { return Runner::small(to, n, ws.t, *p, *g2, 1.f / kPScale, cols); };                          // G = T P
+      if ((s = products(make_p, make_p, 1)) != RT3D_OK) return s;
+      if (more || q) {
+        s = more && q ? products(make_t, make_q, 2) : more ? products(make_t, make_t, 1) : products(make_q, make_q, 1);
+        if (s != RT3D_OK) return s;
+      }
+      if (q) {
         q = &ws.q[q_next];
         q_next ^= 1;
       }
-      if (n && (s = r.small_products(a, n, *p)) != RT3D_OK) return s;
-      if (i + 1 < steps) {                                                                              // G = T P
-        std::memset(&a, 0, sizeof(a));
-        if (!r.small(&a.p[0], ws.t, *p, *g2, 1.f / kPScale)) return RT3D_ERR_CUDA;
-        if ((s = r.small_products(a, 1, *g2)) != RT3D_OK) return s;
+      if (more) {
+        if ((s = products(make_g, make_g, 1)) != RT3D_OK) return s;
         const Matrix* was = g; g = g2; g2 = was;
       }
       if (!q) { q = p; const Matrix* was = p; p = p2; p2 = was; }                                       // the first P is the first Q
     }
     done += steps;
     const bool last = done == plan.steps;
-    ProductArgs a;
-    std::memset(&a, 0, sizeof(a));
-    Problem& c = a.p[0];
-    if (!Runner::maps_of(c.a, *q, kTile) || !Runner::maps_of(c.b, *x, 64)) return RT3D_ERR_CUDA;
-    a.n_problems = 1; a.parts = parts == 2 ? 3 : 2; a.b_rows = 1;
-    a.chunks = ceil_div(x->rows, 64);
-    a.tiles_m = ceil_div(x->rows, kTile); a.tiles_n = ceil_div(x->cols, kTile); a.n_tiles = a.tiles_m * a.tiles_n;
-    a.rows = x->rows; a.cols = x->cols;
-    a.factor = ws.factors + kRuns + run;
-    c.alpha = 1.f / kPScale;
-    if (last) {
-      c.out = res.out; c.alpha /= kXScale;
-      a.turned = res.turned; a.bf = res.bf; a.w = res.w; a.mask = res.mask; a.keep_share = res.keep_share; a.step = res.step; a.w_pitch = res.pitch;
-    } else {
-      c.out = kOutParts; c.c_hi = next->hi; c.c_lo = x_parts[1] == 2 ? next->lo : nullptr; c.pitch = next->pitch;
+    Problem* c = short_x ? chain.add() : &one.p[0];
+    if (!short_x) {
+      if ((s = flush()) != RT3D_OK) return s;
+      std::memset(&one, 0, sizeof(one));
     }
-    if ((s = r.run(a)) != RT3D_OK) return s;
-    const Matrix* was = x; x = next; next = was;
+    if (!Runner::apply(c, *q, *cur, parts, ws.factors + kRuns + run, short_x ? cols : kTile)) return RT3D_ERR_CUDA;
+    if (last) {
+      c->out = res.out; c->alpha /= kXScale;
+    } else {
+      parts = exact ? 2 : later_parts(plan, done);
+      c->out = kOutParts; c->c_hi = other->hi; c->c_lo = parts == 2 ? other->lo : nullptr; c->pitch = other->pitch;
+    }
+    auto results = [&](auto& args) {
+      args.turned = res.turned; args.bf = res.bf; args.w = res.w; args.mask = res.mask;
+      args.keep_share = res.keep_share; args.step = res.step; args.w_pitch = res.pitch;
+    };
+    if (short_x) {
+      chain.end_step();
+      results(chain.a);
+      if (last && (s = flush()) != RT3D_OK) return s;
+    } else {
+      results(one);
+      if ((s = r.run(one, 1)) != RT3D_OK) return s;
+    }
+    const Matrix* was = cur; cur = other; other = was;
   }
   return RT3D_OK;
 }
@@ -808,8 +979,7 @@ rt3d_status orthogonalize(const T* g, int64_t pitch, int m, int k, const Plan& p
   Workspace ws;
   workspace_of(m, k, base, &ws);
   const Result res{kOutDirection, m > k, out, nullptr, nullptr, 0.f, 0.f, (long long)out_pitch};
-  const int parts[2] = {sizeof(T) == 2 ? 1 : 2, 1};
-  return direction(Source<T>{g, pitch, nullptr, nullptr, 0.f, 0}, m, k, plan, 3, parts, ws, res, dev, st);
+  return direction(Source<T>{g, pitch, nullptr, nullptr, 0.f, 0}, m, k, plan, 3, false, ws, res, dev, st);
 }
 
 template <typename T>
@@ -818,8 +988,7 @@ rt3d_status update(float* w, float* momentum, const T* g, const uint8_t* mask, i
   Workspace ws;
   workspace_of(m, k, base, &ws);
   const Result res{kOutUpdate, m > k, nullptr, w, mask, float(1.0 - double(p.lr) * p.weight_decay), float(double(p.lr) * p.scale), k};
-  const int parts[2] = {2, 2};
-  return direction(Source<T>{g, k, momentum, mask, p.mu, p.nesterov}, m, k, plan, 2, parts, ws, res, dev, st);
+  return direction(Source<T>{g, k, momentum, mask, p.mu, p.nesterov}, m, k, plan, 2, true, ws, res, dev, st);
 }
 
 }  // namespace

@@ -208,22 +208,22 @@ split_kernel(Source<T> s, int m, int k, const double* __restrict__ sums, double 
 constexpr int kTile = 128;                           // rows of a tile
 constexpr uint32_t kRowsBytes = kTile * 128;         // of 128 x 64 fp16
 constexpr int kProductThreads = 320;                 // producer, issuer, eight warps for the results
-constexpr uint32_t kRingBytes = 12 * kRowsBytes;
-constexpr uint32_t kProductSmem = kRingBytes + 1024 + sizeof(Barriers);
 constexpr int kMostProblems = 16;                    // of one launch
 
 // Tiles of 128 x kCols: a stage holds 64 of the sum of up to four operands (hi and lo of A and B).
 template <int kCols>
 struct Stage {
   static constexpr uint32_t kColsBytes = kCols * 128, kBAt = 2 * kRowsBytes, kBytes = 2 * kRowsBytes + 2 * kColsBytes;
-  static constexpr int kRing = int(kRingBytes / kBytes);
+  static constexpr int kRing = 3;
+  // results on their way out (128 x 64): hi and lo, and their transposes
+  static constexpr uint32_t kOutAt = kRing * kBytes, kTurnedAt = kOutAt + 2 * kRowsBytes, kAllBytes = kCols == 64 ? kTurnedAt + 2 * kRowsBytes : kRing * kBytes;
 };
 
 enum { kOutParts = 0, kOutDirection = 1, kOutUpdate = 2 };
 
 // One product C = A B: B^T's rows (K-major), or B's own (the last product of a run, X).
+struct Maps { CUtensorMap a[2], b[2], c[2], c_turned[2]; };        // hi and lo; of C where it leaves through shared memory
 struct Problem {
-  CUtensorMap a[2], b[2];                            // hi and lo
   int out;                                           // what becomes of C = alpha * factor * sum + diag I + beta D
   float alpha, beta, diag;
   const float* factor;                               // nullptr: 1
@@ -240,9 +240,14 @@ struct Problem {
 };
 // Products of a launch: the problems [first[s], first[s + 1]) of a step run beside one another, every step after the one before.
 template <int kProblems>
-struct ProductArgs {
+struct Steps {
   Problem p[kProblems];
   int first[kProblems + 1];
+};
+template <int kProblems>
+struct ProductArgs {
+  Maps m[kProblems];
+  Steps<kProblems> steps;
   int n_steps, splits;
   int one_cluster;                                   // the grid is a cluster, which is what steps wait through
   unsigned* arrived;                                 // else: CTAs that have reached the ends of steps, all together
@@ -256,6 +261,9 @@ struct ProductArgs {
   int32_t* err;
 };
 
+template <int kCols>
+constexpr uint32_t kProductSmem = Stage<kCols>::kAllBytes + 1024 + sizeof(Barriers) + sizeof(Steps<kMostProblems>) + 16;
+
 // fp16 x fp16 -> fp32, M = 128, A K-major; B K-major or its own rows.
 template <int kCols>
 __device__ __forceinline__ uint32_t instr_desc_f16(bool b_rows) {
@@ -268,7 +276,7 @@ __device__ __forceinline__ uint64_t smem_desc_rows(uint32_t addr) {
 
 struct TileAt { int problem, i, j; };
 template <int kCols, int kProblems>
-__device__ __forceinline__ TileAt tile_at(const ProductArgs<kProblems>& a, int s, int item) {
+__device__ __forceinline__ TileAt tile_at(const Steps<kProblems>& a, int s, int item) {
   TileAt t;
   t.problem = a.first[s];
   while (item >= a.p[t.problem].n_tiles) item -= a.p[t.problem++].n_tiles;
@@ -288,19 +296,31 @@ __device__ __forceinline__ TileAt tile_at(const ProductArgs<kProblems>& a, int s
 template <int kCols>
 __device__ __forceinline__ bool on_diagonal(const TileAt& t) { return (t.j + 1) * kCols > t.i * kTile; }
 
+// 16 values of D, which are there before the product is.
+struct Addend {
+  uint4 hi[2], lo[2];
+  __device__ __forceinline__ void load(const Problem& p, long long at) {
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+      hi[q] = __ldcg(reinterpret_cast<const uint4*>(p.d_hi + at + 8 * q));
+      lo[q] = __ldcg(reinterpret_cast<const uint4*>(p.d_lo + at + 8 * q));
+    }
+  }
+};
+
 // 16 columns from c0 on of this thread's row of a tile.
 template <int kCols, int kProblems>
-__device__ __forceinline__ void finish16(const ProductArgs<kProblems>& a, const Problem& p, const TileAt& t, int row, int c0, float (&v)[16], float alpha) {
+__device__ __forceinline__ void finish16(const ProductArgs<kProblems>& a, const Problem& p, const TileAt& t, int row, int c0, float (&v)[16], float alpha,
+                                         const Addend& d) {
   const int i = t.i * kTile + row, j = t.j * kCols + c0;
 #pragma unroll
   for (int e = 0; e < 16; ++e) v[e] *= alpha;
   if (p.out == kOutParts) {
     if (p.symmetric) {                               // small matrices, whole tiles
       if (p.d_hi) {
-        const long long at = i * p.pitch + j;
 #pragma unroll
         for (int q = 0; q < 2; ++q) {
-          const uint4 h = __ldcg(reinterpret_cast<const uint4*>(p.d_hi + at + 8 * q)), l = __ldcg(reinterpret_cast<const uint4*>(p.d_lo + at + 8 * q));
+          const uint4 h = d.hi[q], l = d.lo[q];
           const __half2 *hh = reinterpret_cast<const __half2*>(&h), *ll = reinterpret_cast<const __half2*>(&l);
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
@@ -391,8 +411,102 @@ __device__ __forceinline__ void finish16(const ProductArgs<kProblems>& a, const 
   }
 }
 
+__device__ __forceinline__ void tma_store_2d(const CUtensorMap* map, uint32_t src, int c0, int c1) {
+  asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%2, %3}], [%1];"
+               ::"l"(reinterpret_cast<uint64_t>(map)), "r"(src), "r"(c0), "r"(c1) : "memory");
+}
+__device__ __forceinline__ uint4 lds128(uint32_t addr) {
+  uint4 v;
+  asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
+  return v;
+}
+__device__ __forceinline__ void sts128(uint32_t addr, const uint4& v) {
+  asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+}
+
+// The parts of a tile of 128 x 64 through shared memory and out in whole rows, with its transpose where the matrix is symmetric; D comes
+// in the same way, to the places its thread then writes.  (16-byte accesses of a row each, which touch 32 lines, kept the SM's load
+// and store unit busy for 2000 clocks of a step's 8000, the transposes' 2-byte ones for longer.)  Called by all 256 threads; `ok`: the
+// product is there.
+template <int kCols>
+__device__ __forceinline__ void finish_staged(const Problem& p, const Maps& m, const TileAt& t, uint32_t taddr, int row, int half, float alpha, uint32_t base,
+                                              uint32_t tmem_full, uint32_t full_parity, uint32_t d_parity, Barriers* bars, int32_t* err) {
+  typedef Stage<kCols> S;
+  const bool leader = threadIdx.x == 64, add = p.d_hi != nullptr, mirrored = p.symmetric && !on_diagonal<kCols>(t);
+  const uint32_t out = base + S::kOutAt, turned = base + S::kTurnedAt, d_bar = smem_u32(&bars->full[kMaxStages - 1]);
+  if (leader) {
+    tma_store_wait_read_0();
+    if (add) {
+      mbar_expect_tx(d_bar, 2 * kRowsBytes);
+      for (int q = 0; q < 2; ++q) tma_load_2d(out + q * kRowsBytes, &m.a[q], d_bar, t.j * kCols, t.i * kTile);
+    }
+  }
+  bool ok = mbar_wait_warp(tmem_full, full_parity, bars, err, 4);
+  tc_fence_after();
+  epilogue_bar_sync(256);                            // the leader has waited for the last tile's way out
+  if (add) ok = mbar_wait_warp(d_bar, d_parity, bars, err, 6) && ok;
+  if (ok) {
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+      const int c0 = half * 32 + q * 16;
+      uint32_t r[16];
+      __syncwarp();
+      tmem_ld16(taddr + c0, r);
+      float v[16];
+#pragma unroll
+      for (int e = 0; e < 16; ++e) v[e] = alpha * __uint_as_float(r[e]);
+      const uint32_t line = out + row * 128;
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const uint32_t at = line + (((c0 / 8 + u) ^ (row & 7)) << 4);
+        if (add) {
+          const uint4 dh = lds128(at), dl = lds128(at + kRowsBytes);
+          const __half2 *hh = reinterpret_cast<const __half2*>(&dh), *ll = reinterpret_cast<const __half2*>(&dl);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float2 x = __half22float2(hh[e]), y = __half22float2(ll[e]);
+            v[8 * u + 2 * e] += p.beta * (x.x + y.x); v[8 * u + 2 * e + 1] += p.beta * (x.y + y.y);
+          }
+        }
+        if (p.symmetric) {
+          const int i = t.i * kTile + row, j = t.j * kCols + c0 + 8 * u;
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            if (i == j + e) v[8 * u + e] += p.diag;
+        }
+        __half h[8], l[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) split_half(v[8 * u + e], h[e], l[e]);
+        sts128(at, *reinterpret_cast<const uint4*>(h));
+        sts128(at + kRowsBytes, *reinterpret_cast<const uint4*>(l));
+        if (mirrored) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const int j = c0 + 8 * u + e;
+            const uint32_t to = turned + (row >> 6) * 8192 + j * 128 + ((((row & 63) >> 3) ^ (j & 7)) << 4) + (row & 7) * 2;
+            asm volatile("st.shared.u16 [%0], %1;" ::"r"(to), "h"(__half_as_ushort(h[e])) : "memory");
+            asm volatile("st.shared.u16 [%0], %1;" ::"r"(to + kRowsBytes), "h"(__half_as_ushort(l[e])) : "memory");
+          }
+        }
+      }
+    }
+  }
+  asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  epilogue_bar_sync(256);
+  if (leader && ok) {
+    const int parts = p.c_lo ? 2 : 1;
+    for (int q = 0; q < parts; ++q) {
+      tma_store_2d(&m.c[q], out + q * kRowsBytes, t.j * kCols, t.i * kTile);
+      if (mirrored)
+        for (int h = 0; h < 2; ++h) tma_store_2d(&m.c_turned[q], turned + q * kRowsBytes + h * 8192, t.i * kTile + 64 * h, t.j * kCols);
+    }
+    asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+  }
+}
+
 // All CTAs of a cooperative grid have ended the step: `target` arrivals in all.  Bounded like every wait here.
 __device__ __forceinline__ void grid_barrier(unsigned* arrived, unsigned target, Barriers* bars, int32_t* err) {
+  __threadfence();
   __syncwarp();
   __syncthreads();
   if (threadIdx.x == 0) {
@@ -425,7 +539,8 @@ product_kernel(const __grid_constant__ ProductArgs<kProblems> a) {
   typedef Stage<kCols> S;
   extern __shared__ unsigned char smem_raw[];
   const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
-  Barriers* bars = reinterpret_cast<Barriers*>(smem_raw + (base - smem_u32(smem_raw)) + kRingBytes);
+  Barriers* bars = reinterpret_cast<Barriers*>(smem_raw + (base - smem_u32(smem_raw)) + S::kAllBytes);
+  Steps<kProblems>& steps = *reinterpret_cast<Steps<kProblems>*>(bars + 1);
   const int warp = uniform(int(threadIdx.x >> 5)), lane = threadIdx.x & 31;
   const int split = a.splits > 1 ? int(cluster_ctarank()) : 0;
   const int cta = int(blockIdx.x) / a.splits, n_ctas = int(gridDim.x) / a.splits;
@@ -433,13 +548,20 @@ product_kernel(const __grid_constant__ ProductArgs<kProblems> a) {
   if (threadIdx.x == 0) {
     for (int s = 0; s < S::kRing; ++s) { mbar_init(smem_u32(&bars->full[s]), 1); mbar_init(smem_u32(&bars->empty[s]), 1); }
     for (int b = 0; b < 2; ++b) { mbar_init(smem_u32(&bars->tmem_full[b]), 1); mbar_init(smem_u32(&bars->tmem_empty[b]), 8); }
+    mbar_init(smem_u32(&bars->full[kMaxStages - 1]), 1);         // of D
     bars->abort_flag = 0;
     bars->wait_limit = kWaitCycles;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-    for (int p = 0; p < a.first[1]; ++p)
-      for (int q = 0; q < 2; ++q) { tma_prefetch_map(&a.p[p].a[q]); tma_prefetch_map(&a.p[p].b[q]); }
   }
+  // What is read from the parameters on first use costs every step a microsecond: the steps go to shared memory, the descriptors to
+  // their cache.
+  static_assert(sizeof(steps) % 4 == 0, "copied by words");
+  for (int q = int(threadIdx.x); q < int(sizeof(steps) / 4); q += kProductThreads)
+    reinterpret_cast<uint32_t*>(&steps)[q] = reinterpret_cast<const uint32_t*>(&a.steps)[q];
+  if (warp >= 2)
+    for (int q = int(threadIdx.x) - 64; q < a.steps.first[a.n_steps] * (kCols == 64 ? 8 : 4); q += kProductThreads - 64)
+      tma_prefetch_map(kCols == 64 ? &a.m[q >> 3].a[0] + (q & 7) : &a.m[q >> 2].a[0] + (q & 3));
   if (warp == 1) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;"
                  ::"r"(smem_u32(&bars->tmem_base)), "r"(uint32_t(2 * kCols)) : "memory");
@@ -453,18 +575,19 @@ product_kernel(const __grid_constant__ ProductArgs<kProblems> a) {
   pdl_wait();
 
   int stage = 0;                                     // of this role: the ring and the accumulators go on from step to step
-  uint32_t phase = 0, n = 0;
+  uint32_t phase = 0, n = 0, adds = 0;
 #pragma unroll 1
   for (int s = 0; s < a.n_steps; ++s) {
     int n_items = 0;
-    for (int p = a.first[s]; p < a.first[s + 1]; ++p) n_items += a.p[p].n_tiles;
+    for (int p = steps.first[s]; p < steps.first[s + 1]; ++p) n_items += steps.p[p].n_tiles;
     if (warp == 0) {
       // ---------------------------------------------------------------- loads
       if (lane == 0) {
         bool ok = true;
         for (int item = cta; item < n_items && ok; item += n_ctas) {
-          const TileAt t = tile_at<kCols>(a, s, item);
-          const Problem& p = a.p[t.problem];
+          const TileAt t = tile_at<kCols>(steps, s, item);
+          const Problem& p = steps.p[t.problem];
+          const Maps& m = a.m[t.problem];
           const bool one = kCols == kTile && p.same && t.i == t.j;
           const int a_parts = p.parts >= 2 ? 2 : 1, b_parts = one ? 0 : p.parts == 3 ? 2 : 1;
           const int c_last = p.chunks * (split + 1) / a.splits;
@@ -472,14 +595,14 @@ product_kernel(const __grid_constant__ ProductArgs<kProblems> a) {
             const uint32_t full = smem_u32(&bars->full[stage]), at = base + stage * S::kBytes;
             if (!mbar_wait(smem_u32(&bars->empty[stage]), phase ^ 1u, bars, a.err, 1)) { ok = false; break; }
             mbar_expect_tx(full, uint32_t(a_parts) * kRowsBytes + uint32_t(b_parts) * S::kColsBytes);
-            for (int q = 0; q < a_parts; ++q) tma_load_2d(at + q * kRowsBytes, &p.a[q], full, c * 64, t.i * kTile);
+            for (int q = 0; q < a_parts; ++q) tma_load_2d(at + q * kRowsBytes, &m.a[q], full, c * 64, t.i * kTile);
             for (int q = 0; q < b_parts; ++q) {
               const uint32_t to = at + S::kBAt + q * S::kColsBytes;
               if (p.b_rows) {
 #pragma unroll
-                for (int h = 0; h < kCols / 64; ++h) tma_load_2d(to + h * 8192, &p.b[q], full, t.j * kCols + 64 * h, c * 64);
+                for (int h = 0; h < kCols / 64; ++h) tma_load_2d(to + h * 8192, &m.b[q], full, t.j * kCols + 64 * h, c * 64);
               } else {
-                tma_load_2d(to, &p.b[q], full, c * 64, t.j * kCols);
+                tma_load_2d(to, &m.b[q], full, c * 64, t.j * kCols);
               }
             }
             if (++stage == S::kRing) { stage = 0; phase ^= 1u; }
@@ -491,8 +614,8 @@ product_kernel(const __grid_constant__ ProductArgs<kProblems> a) {
       const bool elected = elect_one();
       bool ok = true;
       for (int item = cta; item < n_items && ok; item += n_ctas, ++n) {
-        const TileAt t = tile_at<kCols>(a, s, item);
-        const Problem& p = a.p[t.problem];
+        const TileAt t = tile_at<kCols>(steps, s, item);
+        const Problem& p = steps.p[t.problem];
         const bool one = kCols == kTile && p.same && t.i == t.j;
         const uint32_t idesc = instr_desc_f16<kCols>(p.b_rows != 0);
         const uint64_t b_step = p.b_rows ? (16 * 128) >> 4 : 32 >> 4;           // 16 of the sum
@@ -528,25 +651,35 @@ product_kernel(const __grid_constant__ ProductArgs<kProblems> a) {
       // ---------------------------------------------------------------- results
       const int quad = warp & 3, half = (warp - 2) >> 2, row = quad * 32 + lane;
       for (int item = cta; item < n_items; item += n_ctas, ++n) {
-        const TileAt t = tile_at<kCols>(a, s, item);
-        const Problem& p = a.p[t.problem];
+        const TileAt t = tile_at<kCols>(steps, s, item);
+        const Problem& p = steps.p[t.problem];
         const float alpha = p.factor ? p.alpha * __ldcg(p.factor) : p.alpha;
-        const uint32_t buf = n & 1u;
+        const uint32_t buf = n & 1u, at = tmem + (uint32_t(quad * 32) << 16) + buf * kCols;
+        Addend d;
+        const long long d_at = (t.i * kTile + row) * p.pitch + t.j * kCols;
+        if (kCols == 64 && p.out == kOutParts) {
+          finish_staged<kCols>(p, a.m[t.problem], t, at, row, half, alpha, base, smem_u32(&bars->tmem_full[buf]), (n >> 1) & 1u, adds & 1u, bars, a.err);
+          adds += p.d_hi != nullptr;
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(smem_u32(&bars->tmem_empty[buf]));
+          continue;
+        }
         if (!mbar_wait_warp(smem_u32(&bars->tmem_full[buf]), (n >> 1) & 1u, bars, a.err, 4)) break;
         tc_fence_after();
-        const uint32_t at = tmem + (uint32_t(quad * 32) << 16) + buf * kCols;
         if (a.splits > 1) {          // this CTA's only tile: its part goes where the stages were, which every product has read
           store_partial_row(at, kCols, true, reinterpret_cast<float*>(smem_raw + (base - smem_u32(smem_raw))) + row * kPartRow, half * 32, 64);
         } else {
 #pragma unroll 1
           for (int c0 = half * 16; c0 < kCols; c0 += 32) {
             uint32_t r[16];
+            if (p.d_hi) d.load(p, d_at + c0);
             __syncwarp();
             tmem_ld16(at + c0, r);
             float v[16];
 #pragma unroll
             for (int e = 0; e < 16; ++e) v[e] = __uint_as_float(r[e]);
-            finish16<kCols>(a, p, t, row, c0, v, alpha);
+            finish16<kCols>(a, p, t, row, c0, v, alpha, d);
           }
         }
         tc_fence_before();
@@ -572,22 +705,22 @@ product_kernel(const __grid_constant__ ProductArgs<kProblems> a) {
                   v[4 * e] += x.x; v[4 * e + 1] += x.y; v[4 * e + 2] += x.z; v[4 * e + 3] += x.w;
                 }
               }
-              finish16<kCols>(a, p, t, row, u * 16, v, alpha);
+              if (p.d_hi) d.load(p, d_at + u * 16);
+              finish16<kCols>(a, p, t, row, u * 16, v, alpha, d);
             }
           }
         }
       }
     }
+    if (kCols == 64 && threadIdx.x == 64) tma_store_wait_all();
     if (kProblems > 1 && s + 1 < a.n_steps) {        // what this step has written is what the next one's copies read
-      asm volatile("fence.proxy.async;" ::: "memory");
-      __threadfence();
-      if (a.one_cluster) {
+      if (a.one_cluster) {                           // a release and an acquire of the cluster
         __syncwarp();
         cluster_sync_all();
       } else {
         grid_barrier(a.arrived, unsigned(s + 1) * gridDim.x, bars, a.err);
       }
-      asm volatile("fence.proxy.async;" ::: "memory");
+      if (threadIdx.x == 0) asm volatile("fence.proxy.async;" ::: "memory");
       if (bars->abort_flag) {                        // this CTA's steps end here; the others' waits run out
         if (!a.one_cluster) break;
       }
@@ -717,14 +850,18 @@ struct Runner {
   }
   static bool maps_of(CUtensorMap (&map)[2], const Matrix& x, int box_rows) { return map_of(&map[0], x.hi, x, box_rows) && map_of(&map[1], x.lo, x, box_rows); }
 
+  // C, where it leaves in tiles of 128 x 64
+  static bool out_maps(Maps* m, const Matrix& c, int cols) {
+    return cols != 64 || (maps_of(m->c, c, kTile) && maps_of(m->c_turned, c, 64));
+  }
   // tiles of n x n on and under the diagonal: as wide as 128 rows need, the last row as wide as n
   static int tiles_under(int n, int cols) {
     const int rows = ceil_div(n, kTile), w = kTile / cols;
     return w * (rows - 1) * rows / 2 + (cols == kTile ? rows : ceil_div(n, cols));
   }
   // G = X X^T (of one or two parts)
-  static bool gram(Problem* p, const Matrix& x, int x_parts, const Matrix& g, const float* factor, int cols) {
-    if (!maps_of(p->a, x, kTile) || !maps_of(p->b, x, cols)) return false;
+  static bool gram(Problem* p, Maps* m, const Matrix& x, int x_parts, const Matrix& g, const float* factor, int cols) {
+    if (!maps_of(m->a, x, kTile) || !maps_of(m->b, x, cols) || !out_maps(m, g, cols)) return false;
     p->parts = x_parts == 2 ? 3 : 1; p->same = 1; p->symmetric = 1;
     p->chunks = ceil_div(x.cols, 64);
     p->n_tiles = tiles_under(x.rows, cols);
@@ -734,8 +871,8 @@ struct Runner {
     return true;
   }
   // C = alpha L R of small symmetric matrices of which n x n exist
-  static bool small(Problem* p, int n, const Matrix& l, const Matrix& r, const Matrix& c, float alpha, int cols) {
-    if (!maps_of(p->a, l, kTile) || !maps_of(p->b, r, cols)) return false;
+  static bool small(Problem* p, Maps* m, int n, const Matrix& l, const Matrix& r, const Matrix& c, float alpha, int cols) {
+    if (!maps_of(m->a, l, kTile) || !maps_of(m->b, r, cols) || !out_maps(m, c, cols)) return false;
     p->parts = 3; p->symmetric = 1;
     p->chunks = ceil_div(n, 64);
     p->n_tiles = tiles_under(n, cols);
@@ -744,16 +881,16 @@ struct Runner {
     return true;
   }
   // P = a + b G + c G G
-  static bool polynomial(Problem* p, int n, const Matrix& g, const Matrix& c, const float* abc, int cols) {
-    if (!small(p, n, g, g, c, abc[2] * kPScale / (kGScale * kGScale), cols)) return false;
+  static bool polynomial(Problem* p, Maps* m, int n, const Matrix& g, const Matrix& c, const float* abc, int cols) {
+    if (!small(p, m, n, g, g, c, abc[2] * kPScale / (kGScale * kGScale), cols)) return false;
     p->same = 1;
     p->beta = abc[1] * kPScale / kGScale; p->diag = abc[0] * kPScale;
     p->d_hi = g.hi; p->d_lo = g.lo;
     return true;
   }
   // C = alpha Q X
-  static bool apply(Problem* p, const Matrix& q, const Matrix& x, int x_parts, const float* factor, int cols) {
-    if (!maps_of(p->a, q, kTile) || !maps_of(p->b, x, 64)) return false;
+  static bool apply(Problem* p, Maps* m, const Matrix& q, const Matrix& x, int x_parts, const float* factor, int cols) {
+    if (!maps_of(m->a, q, kTile) || !maps_of(m->b, x, 64)) return false;
     p->parts = x_parts == 2 ? 3 : 2; p->b_rows = 1;
     p->chunks = ceil_div(x.rows, 64);
     p->tiles_m = ceil_div(x.rows, kTile); p->n_tiles = p->tiles_m * ceil_div(x.cols, cols);
@@ -769,11 +906,11 @@ struct Runner {
     const int d = current_device_index();
     if (d < 0) return RT3D_ERR_CUDA;
     if (!attr_done[d].load()) {
-      if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(kProductSmem)) != cudaSuccess) return RT3D_ERR_CUDA;
+      if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(kProductSmem<kCols>)) != cudaSuccess) return RT3D_ERR_CUDA;
       attr_done[d].store(true);
     }
     a.err = dev.err;
-    LaunchSetup ls(dim3(unsigned(grid)), dim3(kProductThreads), kProductSmem, st, cluster);
+    LaunchSetup ls(dim3(unsigned(grid)), dim3(kProductThreads), kProductSmem<kCols>, st, cluster);
     if (cooperative) {
       ls.attr[0].id = cudaLaunchAttributeCooperative;
       ls.attr[0].val.cooperative = 1;
@@ -784,10 +921,10 @@ struct Runner {
   // One step of tiles of 128 x 128, the sums cut where there are few.
   rt3d_status run(ProductArgs<2>& a, int n_problems) const {
     int items = 0;
-    for (int i = 0; i < n_problems; ++i) items += a.p[i].n_tiles;
-    a.first[0] = 0; a.first[1] = n_problems; a.n_steps = 1;
+    for (int i = 0; i < n_problems; ++i) items += a.steps.p[i].n_tiles;
+    a.steps.first[0] = 0; a.steps.first[1] = n_problems; a.n_steps = 1;
     a.splits = 1;
-    while (a.splits < 8 && items * a.splits * 2 <= dev.sm_count && a.p[0].chunks >= 2 * a.splits) a.splits *= 2;
+    while (a.splits < 8 && items * a.splits * 2 <= dev.sm_count && a.steps.p[0].chunks >= 2 * a.splits) a.splits *= 2;
     return launch<kTile>(a, a.splits > 1 ? items * a.splits : items < dev.sm_count ? items : dev.sm_count, unsigned(a.splits), false);
   }
 };
@@ -802,17 +939,16 @@ struct Fused {
     std::memset(&a, 0, sizeof(a));
     n_problems = 0;
   }
-  Problem* add() { return &a.p[n_problems++]; }
-  void end_step() { a.first[++a.n_steps] = n_problems; }
+  void end_step() { a.steps.first[++a.n_steps] = n_problems; }
   // A cluster's wait takes 0.5 us, a grid's 1.5: eight CTAs where going round more often than a grid would costs less than that
   // (a chunk of three products of 128 x 64: 700 clocks).
   rt3d_status run(unsigned* arrived) {
     int most = 1, extra = 0;
     for (int s = 0; s < a.n_steps; ++s) {
       int items = 0;
-      for (int p = a.first[s]; p < a.first[s + 1]; ++p) items += a.p[p].n_tiles;
+      for (int p = a.steps.first[s]; p < a.steps.first[s + 1]; ++p) items += a.steps.p[p].n_tiles;
       most = items > most ? items : most;
-      extra += (ceil_div(items, 8) - ceil_div(items, r.dev.sm_count)) * a.p[a.first[s]].chunks;
+      extra += (ceil_div(items, 8) - ceil_div(items, r.dev.sm_count)) * a.steps.p[a.steps.first[s]].chunks;
     }
     a.splits = 1;
     a.one_cluster = extra * 700 <= a.n_steps * 1900;
@@ -894,30 +1030,33 @@ rt3d_status direction(const Source<T>& src, int m, int k, const Plan& plan, int 
     int q_next = 0;
     if (short_x) {
       if (chain.n_problems + 3 > kMostProblems && (s = flush()) != RT3D_OK) return s;
-      if (!Runner::gram(chain.add(), *cur, parts, *g, ws.factors + run, cols)) return RT3D_ERR_CUDA;
+      const int at = chain.n_problems++;
+      if (!Runner::gram(&chain.a.steps.p[at], &chain.a.m[at], *cur, parts, *g, ws.factors + run, cols)) return RT3D_ERR_CUDA;
       chain.end_step();
     } else {
       std::memset(&one, 0, sizeof(one));
-      if (!Runner::gram(&one.p[0], *cur, parts, *g, ws.factors + run, kTile)) return RT3D_ERR_CUDA;
+      if (!Runner::gram(&one.steps.p[0], &one.m[0], *cur, parts, *g, ws.factors + run, kTile)) return RT3D_ERR_CUDA;
       if ((s = r.run(one, 1)) != RT3D_OK) return s;
     }
     // a step of one or two products
     auto products = [&](auto&& first_product, auto&& second_product, int count) -> rt3d_status {
-      if (n_fused) {
-        if (!first_product(chain.add()) || (count == 2 && !second_product(chain.add()))) return RT3D_ERR_CUDA;
-        chain.end_step();
-        return RT3D_OK;
+      if (!n_fused) std::memset(&one, 0, sizeof(one));
+      for (int i = 0; i < count; ++i) {
+        const int at = n_fused ? chain.n_problems++ : i;
+        Problem* p = n_fused ? &chain.a.steps.p[at] : &one.steps.p[at];
+        Maps* m = n_fused ? &chain.a.m[at] : &one.m[at];
+        if (!(i ? second_product(p, m) : first_product(p, m))) return RT3D_ERR_CUDA;
       }
-      std::memset(&one, 0, sizeof(one));
-      if (!first_product(&one.p[0]) || (count == 2 && !second_product(&one.p[1]))) return RT3D_ERR_CUDA;
-      return r.run(one, count);
+      if (!n_fused) return r.run(one, count);
+      chain.end_step();
+      return RT3D_OK;
     };
     for (int i = 0; i < steps; ++i) {
       const bool more = i + 1 < steps;
-      auto make_p = [&](Problem* to) { return Runner::polynomial(to, n, *g, *p, plan.abc[done + i], cols); };
-      auto make_t = [&](Problem* to) { return Runner::small(to, n, *p, *g, ws.t, kGScale / (kPScale * kGScale), cols); };           // T = P G
-      auto make_q = [&](Problem* to) { return Runner::small(to, n, *p, *q, ws.q[q_next], 1.f / kPScale, cols); };                   // Q = P Q
-      auto make_g = [&](Problem* to) { return Runner::small(to, n, ws.t, *p, *g2, 1.f / kPScale, cols); };                          // G = T P
+      auto make_p = [&](Problem* to, Maps* maps) { return Runner::polynomial(to, maps, n, *g, *p, plan.abc[done + i], cols); };
+      auto make_t = [&](Problem* to, Maps* maps) { return Runner::small(to, maps, n, *p, *g, ws.t, kGScale / (kPScale * kGScale), cols); };           // T = P G
+      auto make_q = [&](Problem* to, Maps* maps) { return Runner::small(to, maps, n, *p, *q, ws.q[q_next], 1.f / kPScale, cols); };                   // Q = P Q
+      auto make_g = [&](Problem* to, Maps* maps) { return Runner::small(to, maps, n, ws.t, *p, *g2, 1.f / kPScale, cols); };                          // G = T P
       if ((s = products(make_p, make_p, 1)) != RT3D_OK) return s;
       if (more || q) {
         s = more && q ? products(make_t, make_q, 2) : more ? products(make_t, make_t, 1) : products(make_q, make_q, 1);
@@ -935,15 +1074,17 @@ rt3d_status direction(const Source<T>& src, int m, int k, const Plan& plan, int 
     }
     done += steps;
     const bool last = done == plan.steps;
-    Problem* c = short_x ? chain.add() : &one.p[0];
+    Problem* c = short_x ? &chain.a.steps.p[chain.n_problems] : &one.steps.p[0];
+    Maps* c_maps = short_x ? &chain.a.m[chain.n_problems++] : &one.m[0];
     if (!short_x) {
       if ((s = flush()) != RT3D_OK) return s;
       std::memset(&one, 0, sizeof(one));
     }
-    if (!Runner::apply(c, *q, *cur, parts, ws.factors + kRuns + run, short_x ? cols : kTile)) return RT3D_ERR_CUDA;
+    if (!Runner::apply(c, c_maps, *q, *cur, parts, ws.factors + kRuns + run, short_x ? cols : kTile)) return RT3D_ERR_CUDA;
     if (last) {
       c->out = res.out; c->alpha /= kXScale;
     } else {
+      if (!Runner::out_maps(c_maps, *other, short_x ? cols : kTile)) return RT3D_ERR_CUDA;
       parts = exact ? 2 : later_parts(plan, done);
       c->out = kOutParts; c->c_hi = other->hi; c->c_lo = parts == 2 ? other->lo : nullptr; c->pitch = other->pitch;
     }

@@ -122,6 +122,12 @@ square_sums_kernel(Source<T> s, int m, int k, double* __restrict__ sums) {
   }
 }
 
+// Two values at a time: a conversion of one takes as long as one of two, on a pipe of 16 lanes a clock.
+__device__ __forceinline__ void split_half2(float x, float y, __half2& hi, __half2& lo) {
+  hi = __floats2half2_rn(x, y);
+  const float2 back = __half22float2(hi);
+  lo = __floats2half2_rn(x - back.x, y - back.y);
+}
 __device__ __forceinline__ void split_half(float v, __half& hi, __half& lo) {
   hi = __float2half_rn(v);
   lo = __float2half_rn(v - __half2float(hi));
@@ -178,13 +184,14 @@ split_kernel(Source<T> s, int m, int k, const double* __restrict__ sums, double 
       for (int e = 0; e < 4; ++e) tile[r][lane * 4 + e] = v[e];
       continue;
     }
-    __half h[4], l[4];
+    __half2 h2[2], l2[2];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) split_half(v[e], h[e], l[e]);
+    for (int e = 0; e < 2; ++e) split_half2(v[2 * e], v[2 * e + 1], h2[e], l2[e]);
+    const __half *h = reinterpret_cast<const __half*>(h2), *l = reinterpret_cast<const __half*>(l2);
     __half *to = hi + i * x_pitch + j, *lo_to = lo + i * x_pitch + j;
     if (j + 4 <= k) {                                            // the pitch is a multiple of 8
-      *reinterpret_cast<uint2*>(to) = *reinterpret_cast<const uint2*>(h);
-      if (lo) *reinterpret_cast<uint2*>(lo_to) = *reinterpret_cast<const uint2*>(l);
+      *reinterpret_cast<uint2*>(to) = *reinterpret_cast<const uint2*>(h2);
+      if (lo) *reinterpret_cast<uint2*>(lo_to) = *reinterpret_cast<const uint2*>(l2);
     } else {
       for (int e = 0; e < 4 && j + e < k; ++e) {
         to[e] = h[e];
@@ -215,14 +222,17 @@ template <int kCols>
 struct Stage {
   static constexpr uint32_t kColsBytes = kCols * 128, kBAt = 2 * kRowsBytes, kBytes = 2 * kRowsBytes + 2 * kColsBytes;
   static constexpr int kRing = 3;
-  // results on their way out (128 x 64): hi and lo, and their transposes
-  static constexpr uint32_t kOutAt = kRing * kBytes, kTurnedAt = kOutAt + 2 * kRowsBytes, kAllBytes = kCols == 64 ? kTurnedAt + 2 * kRowsBytes : kRing * kBytes;
+  // results on their way out (128 x 64): hi and lo
+  static constexpr uint32_t kOutAt = kRing * kBytes, kAllBytes = kCols == 64 ? kOutAt + 2 * kRowsBytes : kRing * kBytes;
 };
 
 enum { kOutParts = 0, kOutDirection = 1, kOutUpdate = 2 };
 
-// One product C = A B: B^T's rows (K-major), or B's own (the last product of a run, X).
-struct Maps { CUtensorMap a[2], b[2], c[2], c_turned[2]; };        // hi and lo; of C where it leaves through shared memory
+// One product C = A B from A's rows and B^T's (K-major operands), or B's own (X, the last product of a run).  Of a symmetric matrix only
+// the 128 x 128 blocks on and under the diagonal are there: what a row has above them is the transpose of a block under the diagonal and
+// enters the product as such.
+// Boxes of 64 columns, hi and lo: 128 rows of A, kCols of B, 64 of either, and 128 of C where it leaves through shared memory.
+struct Maps { CUtensorMap a[2], b[2], a64[2], b64[2], c[2]; };
 struct Problem {
   int out;                                           // what becomes of C = alpha * factor * sum + diag I + beta D
   float alpha, beta, diag;
@@ -232,8 +242,9 @@ struct Problem {
   long long pitch;                                   // of C and D
   int parts;                                         // 1: hi hi; 2: hi hi + lo hi; 3: and hi lo
   int same;                                          // A and B are the same matrix: a tile on the diagonal loads it once
+  int a_under, b_under;                              // A, B is symmetric and lies on and under the diagonal only
   int b_rows;                                        // B's own rows
-  int symmetric;                                     // tiles on and under the diagonal, mirrored
+  int symmetric;                                     // so is C: tiles on and under the diagonal
   int chunks;
   int tiles_m, n_tiles;
   int rows, cols;                                    // what of C exists (symmetric: all of the tiles)
@@ -264,17 +275,19 @@ struct ProductArgs {
 template <int kCols>
 constexpr uint32_t kProductSmem = Stage<kCols>::kAllBytes + 1024 + sizeof(Barriers) + sizeof(Steps<kMostProblems>) + 16;
 
-// fp16 x fp16 -> fp32, M = 128, A K-major; B K-major or its own rows.
+// fp16 x fp16 -> fp32, M = 128; A K-major or transposed, B K-major or its own rows.
 template <int kCols>
-__device__ __forceinline__ uint32_t instr_desc_f16(bool b_rows) {
-  return (1u << 4) | (b_rows ? 1u << 16 : 0u) | (uint32_t(kCols >> 3) << 17) | (uint32_t(kTile >> 4) << 24);
+__device__ __forceinline__ uint32_t instr_desc_f16(bool a_turned, bool b_rows) {
+  return (1u << 4) | (a_turned ? 1u << 15 : 0u) | (b_rows ? 1u << 16 : 0u) | (uint32_t(kCols >> 3) << 17) | (uint32_t(kTile >> 4) << 24);
 }
-// B's own rows: 64 columns (128 bytes, swizzled) by rows of the sum; 8 rows 1024 bytes apart, 64 columns 8192.
+// Rows along the sum: 64 columns (128 bytes, swizzled) by rows of the sum; 8 rows 1024 bytes apart, 64 columns 8192.
 __device__ __forceinline__ uint64_t smem_desc_rows(uint32_t addr) {
   return uint64_t((addr & 0x3FFFFu) >> 4) | uint64_t(8192 >> 4) << 16 | uint64_t(1024 >> 4) << 32 | uint64_t(1) << 46 | uint64_t(2) << 61;
 }
 
 struct TileAt { int problem, i, j; };
+// Whether chunk c of the rows `at`.. of a symmetric matrix lies above the blocks that are there.
+__device__ __forceinline__ bool above(int under, int c, int at) { return under && c * 64 >= (at / kTile + 1) * kTile; }
 template <int kCols, int kProblems>
 __device__ __forceinline__ TileAt tile_at(const Steps<kProblems>& a, int s, int item) {
   TileAt t;
@@ -293,9 +306,6 @@ __device__ __forceinline__ TileAt tile_at(const Steps<kProblems>& a, int s, int 
   }
   return t;
 }
-template <int kCols>
-__device__ __forceinline__ bool on_diagonal(const TileAt& t) { return (t.j + 1) * kCols > t.i * kTile; }
-
 // 16 values of D, which are there before the product is.
 struct Addend {
   uint4 hi[2], lo[2];
@@ -335,9 +345,9 @@ __device__ __forceinline__ void finish16(const ProductArgs<kProblems>& a, const 
     } else if (i >= p.rows) {
       return;
     }
-    __half h[16], l[16];
+    __half2 h[8], l[8];
 #pragma unroll
-    for (int e = 0; e < 16; ++e) split_half(v[e], h[e], l[e]);
+    for (int e = 0; e < 8; ++e) split_half2(v[2 * e], v[2 * e + 1], h[e], l[e]);
     const long long at = i * p.pitch + j;
 #pragma unroll
     for (int q = 0; q < 2; ++q)
@@ -345,13 +355,6 @@ __device__ __forceinline__ void finish16(const ProductArgs<kProblems>& a, const 
         *reinterpret_cast<uint4*>(p.c_hi + at + 8 * q) = reinterpret_cast<const uint4*>(h)[q];
         if (p.c_lo) *reinterpret_cast<uint4*>(p.c_lo + at + 8 * q) = reinterpret_cast<const uint4*>(l)[q];
       }
-    if (p.symmetric && !on_diagonal<kCols>(t)) {
-#pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        p.c_hi[(j + e) * p.pitch + i] = h[e];
-        p.c_lo[(j + e) * p.pitch + i] = l[e];
-      }
-    }
     return;
   }
   if (i >= p.rows) return;
@@ -424,16 +427,15 @@ __device__ __forceinline__ void sts128(uint32_t addr, const uint4& v) {
   asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
 }
 
-// The parts of a tile of 128 x 64 through shared memory and out in whole rows, with its transpose where the matrix is symmetric; D comes
-// in the same way, to the places its thread then writes.  (16-byte accesses of a row each, which touch 32 lines, kept the SM's load
-// and store unit busy for 2000 clocks of a step's 8000, the transposes' 2-byte ones for longer.)  Called by all 256 threads; `ok`: the
-// product is there.
+// The parts of a tile of 128 x 64 through shared memory and out in whole rows; D comes the same way, to the places its thread then
+// writes.  (16-byte accesses of a row each, which touch 32 lines, kept the SM's load and store unit busy for 2000 clocks of a
+// step's 8000.)  Called by all 256 threads.
 template <int kCols>
 __device__ __forceinline__ void finish_staged(const Problem& p, const Maps& m, const TileAt& t, uint32_t taddr, int row, int half, float alpha, uint32_t base,
                                               uint32_t tmem_full, uint32_t full_parity, uint32_t d_parity, Barriers* bars, int32_t* err) {
   typedef Stage<kCols> S;
-  const bool leader = threadIdx.x == 64, add = p.d_hi != nullptr, mirrored = p.symmetric && !on_diagonal<kCols>(t);
-  const uint32_t out = base + S::kOutAt, turned = base + S::kTurnedAt, d_bar = smem_u32(&bars->full[kMaxStages - 1]);
+  const bool leader = threadIdx.x == 64, add = p.d_hi != nullptr;
+  const uint32_t out = base + S::kOutAt, d_bar = smem_u32(&bars->full[kMaxStages - 1]);
   if (leader) {
     tma_store_wait_read_0();
     if (add) {
@@ -474,20 +476,11 @@ __device__ __forceinline__ void finish_staged(const Problem& p, const Maps& m, c
           for (int e = 0; e < 8; ++e)
             if (i == j + e) v[8 * u + e] += p.diag;
         }
-        __half h[8], l[8];
+        __half2 h[4], l[4];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) split_half(v[8 * u + e], h[e], l[e]);
+        for (int e = 0; e < 4; ++e) split_half2(v[8 * u + 2 * e], v[8 * u + 2 * e + 1], h[e], l[e]);
         sts128(at, *reinterpret_cast<const uint4*>(h));
         sts128(at + kRowsBytes, *reinterpret_cast<const uint4*>(l));
-        if (mirrored) {
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            const int j = c0 + 8 * u + e;
-            const uint32_t to = turned + (row >> 6) * 8192 + j * 128 + ((((row & 63) >> 3) ^ (j & 7)) << 4) + (row & 7) * 2;
-            asm volatile("st.shared.u16 [%0], %1;" ::"r"(to), "h"(__half_as_ushort(h[e])) : "memory");
-            asm volatile("st.shared.u16 [%0], %1;" ::"r"(to + kRowsBytes), "h"(__half_as_ushort(l[e])) : "memory");
-          }
-        }
       }
     }
   }
@@ -495,11 +488,7 @@ __device__ __forceinline__ void finish_staged(const Problem& p, const Maps& m, c
   epilogue_bar_sync(256);
   if (leader && ok) {
     const int parts = p.c_lo ? 2 : 1;
-    for (int q = 0; q < parts; ++q) {
-      tma_store_2d(&m.c[q], out + q * kRowsBytes, t.j * kCols, t.i * kTile);
-      if (mirrored)
-        for (int h = 0; h < 2; ++h) tma_store_2d(&m.c_turned[q], turned + q * kRowsBytes + h * 8192, t.i * kTile + 64 * h, t.j * kCols);
-    }
+    for (int q = 0; q < parts; ++q) tma_store_2d(&m.c[q], out + q * kRowsBytes, t.j * kCols, t.i * kTile);
     asm volatile("cp.async.bulk.commit_group;" ::: "memory");
   }
 }
@@ -560,8 +549,7 @@ product_kernel(const __grid_constant__ ProductArgs<kProblems> a) {
   for (int q = int(threadIdx.x); q < int(sizeof(steps) / 4); q += kProductThreads)
     reinterpret_cast<uint32_t*>(&steps)[q] = reinterpret_cast<const uint32_t*>(&a.steps)[q];
   if (warp >= 2)
-    for (int q = int(threadIdx.x) - 64; q < a.steps.first[a.n_steps] * (kCols == 64 ? 8 : 4); q += kProductThreads - 64)
-      tma_prefetch_map(kCols == 64 ? &a.m[q >> 3].a[0] + (q & 7) : &a.m[q >> 2].a[0] + (q & 3));
+    for (int q = int(threadIdx.x) - 64; q < a.steps.first[a.n_steps] * 10; q += kProductThreads - 64) tma_prefetch_map(&a.m[0].a[0] + q);
   if (warp == 1) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;"
                  ::"r"(smem_u32(&bars->tmem_base)), "r"(uint32_t(2 * kCols)) : "memory");
@@ -595,12 +583,21 @@ product_kernel(const __grid_constant__ ProductArgs<kProblems> a) {
             const uint32_t full = smem_u32(&bars->full[stage]), at = base + stage * S::kBytes;
             if (!mbar_wait(smem_u32(&bars->empty[stage]), phase ^ 1u, bars, a.err, 1)) { ok = false; break; }
             mbar_expect_tx(full, uint32_t(a_parts) * kRowsBytes + uint32_t(b_parts) * S::kColsBytes);
-            for (int q = 0; q < a_parts; ++q) tma_load_2d(at + q * kRowsBytes, &m.a[q], full, c * 64, t.i * kTile);
+            const bool a_turned = above(p.a_under, c, t.i * kTile), b_turned = p.b_rows || above(p.b_under, c, t.j * kCols);
+            for (int q = 0; q < a_parts; ++q) {
+              const uint32_t to = at + q * kRowsBytes;
+              if (a_turned) {
+                tma_load_2d(to, &m.a64[q], full, t.i * kTile, c * 64);
+                tma_load_2d(to + 8192, &m.a64[q], full, t.i * kTile + 64, c * 64);
+              } else {
+                tma_load_2d(to, &m.a[q], full, c * 64, t.i * kTile);
+              }
+            }
             for (int q = 0; q < b_parts; ++q) {
               const uint32_t to = at + S::kBAt + q * S::kColsBytes;
-              if (p.b_rows) {
+              if (b_turned) {
 #pragma unroll
-                for (int h = 0; h < kCols / 64; ++h) tma_load_2d(to + h * 8192, &m.b[q], full, t.j * kCols + 64 * h, c * 64);
+                for (int h = 0; h < kCols / 64; ++h) tma_load_2d(to + h * 8192, &m.b64[q], full, t.j * kCols + 64 * h, c * 64);
               } else {
                 tma_load_2d(to, &m.b[q], full, c * 64, t.j * kCols);
               }
@@ -617,8 +614,6 @@ product_kernel(const __grid_constant__ ProductArgs<kProblems> a) {
         const TileAt t = tile_at<kCols>(steps, s, item);
         const Problem& p = steps.p[t.problem];
         const bool one = kCols == kTile && p.same && t.i == t.j;
-        const uint32_t idesc = instr_desc_f16<kCols>(p.b_rows != 0);
-        const uint64_t b_step = p.b_rows ? (16 * 128) >> 4 : 32 >> 4;           // 16 of the sum
         const uint32_t buf = n & 1u, d = tmem + buf * kCols;
         if (!mbar_wait_warp(smem_u32(&bars->tmem_empty[buf]), ((n >> 1) & 1u) ^ 1u, bars, a.err, 2)) break;
         tc_fence_after();
@@ -627,18 +622,22 @@ product_kernel(const __grid_constant__ ProductArgs<kProblems> a) {
           if (!mbar_wait_warp(smem_u32(&bars->full[stage]), phase, bars, a.err, 3)) { ok = false; break; }
           tc_fence_after();
           const uint32_t at = base + stage * S::kBytes, b_at = one ? at : at + S::kBAt, b_lo_at = one ? at + kRowsBytes : b_at + S::kColsBytes;
-          const uint64_t a_hi = smem_desc_sw128(at), a_lo = smem_desc_sw128(at + kRowsBytes);
-          const uint64_t b_hi = p.b_rows ? smem_desc_rows(b_at) : smem_desc_sw128(b_at);
-          const uint64_t b_lo = p.b_rows ? smem_desc_rows(b_lo_at) : smem_desc_sw128(b_lo_at);
+          const bool a_turned = above(p.a_under, c, t.i * kTile), b_turned = p.b_rows || above(p.b_under, c, t.j * kCols);
+          const uint32_t idesc = instr_desc_f16<kCols>(a_turned, b_turned);
+          const uint64_t a_step = a_turned ? (16 * 128) >> 4 : 32 >> 4, b_step = b_turned ? (16 * 128) >> 4 : 32 >> 4;      // 16 of the sum
+          const uint64_t a_hi = a_turned ? smem_desc_rows(at) : smem_desc_sw128(at);
+          const uint64_t a_lo = a_turned ? smem_desc_rows(at + kRowsBytes) : smem_desc_sw128(at + kRowsBytes);
+          const uint64_t b_hi = b_turned ? smem_desc_rows(b_at) : smem_desc_sw128(b_at);
+          const uint64_t b_lo = b_turned ? smem_desc_rows(b_lo_at) : smem_desc_sw128(b_lo_at);
           if (elected) {
             if (p.parts >= 2)
 #pragma unroll
-              for (int k = 0; k < 4; ++k) umma_bf16(d, a_lo + 2 * k, b_hi + b_step * k, idesc, c > c_first || k ? 1u : 0u);
+              for (int k = 0; k < 4; ++k) umma_bf16(d, a_lo + a_step * k, b_hi + b_step * k, idesc, c > c_first || k ? 1u : 0u);
             if (p.parts == 3)
 #pragma unroll
-              for (int k = 0; k < 4; ++k) umma_bf16(d, a_hi + 2 * k, b_lo + b_step * k, idesc, 1u);
+              for (int k = 0; k < 4; ++k) umma_bf16(d, a_hi + a_step * k, b_lo + b_step * k, idesc, 1u);
 #pragma unroll
-            for (int k = 0; k < 4; ++k) umma_bf16(d, a_hi + 2 * k, b_hi + b_step * k, idesc, c > c_first || k || p.parts >= 2 ? 1u : 0u);
+            for (int k = 0; k < 4; ++k) umma_bf16(d, a_hi + a_step * k, b_hi + b_step * k, idesc, c > c_first || k || p.parts >= 2 ? 1u : 0u);
             umma_commit(smem_u32(&bars->empty[stage]));
           }
           if (++stage == S::kRing) { stage = 0; phase ^= 1u; }
@@ -712,20 +711,22 @@ product_kernel(const __grid_constant__ ProductArgs<kProblems> a) {
         }
       }
     }
-    if (kCols == 64 && threadIdx.x == 64) tma_store_wait_all();
-    if (kProblems > 1 && s + 1 < a.n_steps) {        // what this step has written is what the next one's copies read
+    if (kProblems > 1 && s + 1 < a.n_steps) {
+      // What this step has written is what the next one's copies read: both through the same proxy, so that once the stores are
+      // complete (which this waits for) the barrier orders the two.
+      if (threadIdx.x == 64) tma_store_wait_all();
       if (a.one_cluster) {                           // a release and an acquire of the cluster
         __syncwarp();
         cluster_sync_all();
       } else {
         grid_barrier(a.arrived, unsigned(s + 1) * gridDim.x, bars, a.err);
       }
-      if (threadIdx.x == 0) asm volatile("fence.proxy.async;" ::: "memory");
       if (bars->abort_flag) {                        // this CTA's steps end here; the others' waits run out
         if (!a.one_cluster) break;
       }
     }
   }
+  if (kCols == 64 && threadIdx.x == 64) tma_store_wait_all();
   if (a.splits > 1) {
     // the results' warps have waited once, the others not; and nobody leaves while its part is still being read
     __syncwarp();
@@ -851,9 +852,7 @@ struct Runner {
   static bool maps_of(CUtensorMap (&map)[2], const Matrix& x, int box_rows) { return map_of(&map[0], x.hi, x, box_rows) && map_of(&map[1], x.lo, x, box_rows); }
 
   // C, where it leaves in tiles of 128 x 64
-  static bool out_maps(Maps* m, const Matrix& c, int cols) {
-    return cols != 64 || (maps_of(m->c, c, kTile) && maps_of(m->c_turned, c, 64));
-  }
+  static bool out_maps(Maps* m, const Matrix& c, int cols) { return cols != 64 || maps_of(m->c, c, kTile); }
   // tiles of n x n on and under the diagonal: as wide as 128 rows need, the last row as wide as n
   static int tiles_under(int n, int cols) {
     const int rows = ceil_div(n, kTile), w = kTile / cols;
@@ -872,8 +871,8 @@ struct Runner {
   }
   // C = alpha L R of small symmetric matrices of which n x n exist
   static bool small(Problem* p, Maps* m, int n, const Matrix& l, const Matrix& r, const Matrix& c, float alpha, int cols) {
-    if (!maps_of(m->a, l, kTile) || !maps_of(m->b, r, cols) || !out_maps(m, c, cols)) return false;
-    p->parts = 3; p->symmetric = 1;
+    if (!maps_of(m->a, l, kTile) || !maps_of(m->b, r, cols) || !maps_of(m->a64, l, 64) || !maps_of(m->b64, r, 64) || !out_maps(m, c, cols)) return false;
+    p->parts = 3; p->symmetric = 1; p->a_under = p->b_under = 1;
     p->chunks = ceil_div(n, 64);
     p->n_tiles = tiles_under(n, cols);
     p->rows = p->cols = c.rows;
@@ -890,8 +889,8 @@ struct Runner {
   }
   // C = alpha Q X
   static bool apply(Problem* p, Maps* m, const Matrix& q, const Matrix& x, int x_parts, const float* factor, int cols) {
-    if (!maps_of(m->a, q, kTile) || !maps_of(m->b, x, 64)) return false;
-    p->parts = x_parts == 2 ? 3 : 2; p->b_rows = 1;
+    if (!maps_of(m->a, q, kTile) || !maps_of(m->a64, q, 64) || !maps_of(m->b64, x, 64)) return false;
+    p->parts = x_parts == 2 ? 3 : 2; p->a_under = 1; p->b_rows = 1;
     p->chunks = ceil_div(x.rows, 64);
     p->tiles_m = ceil_div(x.rows, kTile); p->n_tiles = p->tiles_m * ceil_div(x.cols, cols);
     p->rows = x.rows; p->cols = x.cols;

@@ -231,8 +231,11 @@ enum { kOutParts = 0, kOutDirection = 1, kOutUpdate = 2 };
 // One product C = A B from A's rows and B^T's (K-major operands), or B's own (X, the last product of a run).  Of a symmetric matrix only
 // the 128 x 128 blocks on and under the diagonal are there: what a row has above them is the transpose of a block under the diagonal and
 // enters the product as such.
-// Boxes of 64 columns, hi and lo: 128 rows of A, kCols of B, 64 of either, and 128 of C where it leaves through shared memory.
-struct Maps { CUtensorMap a[2], b[2], a64[2], b64[2], c[2]; };
+// The descriptors of a matrix in the workspace, hi and lo: boxes of 64 columns by 128 and by 64 rows.  One table of them serves all
+// products of a call: the few descriptors that a launch uses stay in their cache, where a set for every product made each
+// copy wait for its own (2000 clocks of a step's 6500).
+enum { kX0, kX1, kG0, kG1, kP0, kP1, kT, kQ0, kQ1, kMatrices };
+struct Maps { CUtensorMap rows128[2], rows64[2]; };
 struct Problem {
   int out;                                           // what becomes of C = alpha * factor * sum + diag I + beta D
   float alpha, beta, diag;
@@ -242,6 +245,7 @@ struct Problem {
   long long pitch;                                   // of C and D
   int parts;                                         // 1: hi hi; 2: hi hi + lo hi; 3: and hi lo
   int same;                                          // A and B are the same matrix: a tile on the diagonal loads it once
+  int a, b, c;                                       // the matrices; c < 0: none of them
   int a_under, b_under;                              // A, B is symmetric and lies on and under the diagonal only
   int b_rows;                                        // B's own rows
   int symmetric;                                     // so is C: tiles on and under the diagonal
@@ -257,7 +261,7 @@ struct Steps {
 };
 template <int kProblems>
 struct ProductArgs {
-  Maps m[kProblems];
+  Maps m[kMatrices];
   Steps<kProblems> steps;
   int n_steps, splits;
   int one_cluster;                                   // the grid is a cluster, which is what steps wait through
@@ -431,7 +435,7 @@ __device__ __forceinline__ void sts128(uint32_t addr, const uint4& v) {
 // writes.  (16-byte accesses of a row each, which touch 32 lines, kept the SM's load and store unit busy for 2000 clocks of a
 // step's 8000.)  Called by all 256 threads.
 template <int kCols>
-__device__ __forceinline__ void finish_staged(const Problem& p, const Maps& m, const TileAt& t, uint32_t taddr, int row, int half, float alpha, uint32_t base,
+__device__ __forceinline__ void finish_staged(const Problem& p, const Maps* maps, const TileAt& t, uint32_t taddr, int row, int half, float alpha, uint32_t base,
                                               uint32_t tmem_full, uint32_t full_parity, uint32_t d_parity, Barriers* bars, int32_t* err) {
   typedef Stage<kCols> S;
   const bool leader = threadIdx.x == 64, add = p.d_hi != nullptr;
@@ -440,7 +444,7 @@ __device__ __forceinline__ void finish_staged(const Problem& p, const Maps& m, c
     tma_store_wait_read_0();
     if (add) {
       mbar_expect_tx(d_bar, 2 * kRowsBytes);
-      for (int q = 0; q < 2; ++q) tma_load_2d(out + q * kRowsBytes, &m.a[q], d_bar, t.j * kCols, t.i * kTile);
+      for (int q = 0; q < 2; ++q) tma_load_2d(out + q * kRowsBytes, &maps[p.a].rows128[q], d_bar, t.j * kCols, t.i * kTile);
     }
   }
   bool ok = mbar_wait_warp(tmem_full, full_parity, bars, err, 4);
@@ -488,7 +492,7 @@ __device__ __forceinline__ void finish_staged(const Problem& p, const Maps& m, c
   epilogue_bar_sync(256);
   if (leader && ok) {
     const int parts = p.c_lo ? 2 : 1;
-    for (int q = 0; q < parts; ++q) tma_store_2d(&m.c[q], out + q * kRowsBytes, t.j * kCols, t.i * kTile);
+    for (int q = 0; q < parts; ++q) tma_store_2d(&maps[p.c].rows128[q], out + q * kRowsBytes, t.j * kCols, t.i * kTile);
     asm volatile("cp.async.bulk.commit_group;" ::: "memory");
   }
 }
@@ -543,13 +547,12 @@ product_kernel(const __grid_constant__ ProductArgs<kProblems> a) {
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   }
-  // What is read from the parameters on first use costs every step a microsecond: the steps go to shared memory, the descriptors to
-  // their cache.
+  // What is read from the parameters on first use makes every step wait: the steps go to shared memory, the descriptors to their cache.
   static_assert(sizeof(steps) % 4 == 0, "copied by words");
   for (int q = int(threadIdx.x); q < int(sizeof(steps) / 4); q += kProductThreads)
     reinterpret_cast<uint32_t*>(&steps)[q] = reinterpret_cast<const uint32_t*>(&a.steps)[q];
   if (warp >= 2)
-    for (int q = int(threadIdx.x) - 64; q < a.steps.first[a.n_steps] * 10; q += kProductThreads - 64) tma_prefetch_map(&a.m[0].a[0] + q);
+    for (int q = int(threadIdx.x) - 64; q < (kProblems > 1 ? kMatrices * 4 : 0); q += kProductThreads - 64) tma_prefetch_map(&a.m[0].rows128[0] + q);
   if (warp == 1) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;"
                  ::"r"(smem_u32(&bars->tmem_base)), "r"(uint32_t(2 * kCols)) : "memory");
@@ -575,7 +578,8 @@ product_kernel(const __grid_constant__ ProductArgs<kProblems> a) {
         for (int item = cta; item < n_items && ok; item += n_ctas) {
           const TileAt t = tile_at<kCols>(steps, s, item);
           const Problem& p = steps.p[t.problem];
-          const Maps& m = a.m[t.problem];
+          const Maps &ma = a.m[p.a], &mb = a.m[p.b];
+          const CUtensorMap* b_maps = kCols == 64 ? mb.rows64 : mb.rows128;
           const bool one = kCols == kTile && p.same && t.i == t.j;
           const int a_parts = p.parts >= 2 ? 2 : 1, b_parts = one ? 0 : p.parts == 3 ? 2 : 1;
           const int c_last = p.chunks * (split + 1) / a.splits;
@@ -587,19 +591,19 @@ product_kernel(const __grid_constant__ ProductArgs<kProblems> a) {
             for (int q = 0; q < a_parts; ++q) {
               const uint32_t to = at + q * kRowsBytes;
               if (a_turned) {
-                tma_load_2d(to, &m.a64[q], full, t.i * kTile, c * 64);
-                tma_load_2d(to + 8192, &m.a64[q], full, t.i * kTile + 64, c * 64);
+                tma_load_2d(to, &ma.rows64[q], full, t.i * kTile, c * 64);
+                tma_load_2d(to + 8192, &ma.rows64[q], full, t.i * kTile + 64, c * 64);
               } else {
-                tma_load_2d(to, &m.a[q], full, c * 64, t.i * kTile);
+                tma_load_2d(to, &ma.rows128[q], full, c * 64, t.i * kTile);
               }
             }
             for (int q = 0; q < b_parts; ++q) {
               const uint32_t to = at + S::kBAt + q * S::kColsBytes;
               if (b_turned) {
 #pragma unroll
-                for (int h = 0; h < kCols / 64; ++h) tma_load_2d(to + h * 8192, &m.b64[q], full, t.j * kCols + 64 * h, c * 64);
+                for (int h = 0; h < kCols / 64; ++h) tma_load_2d(to + h * 8192, &mb.rows64[q], full, t.j * kCols + 64 * h, c * 64);
               } else {
-                tma_load_2d(to, &m.b[q], full, c * 64, t.j * kCols);
+                tma_load_2d(to, &b_maps[q], full, c * 64, t.j * kCols);
               }
             }
             if (++stage == S::kRing) { stage = 0; phase ^= 1u; }
@@ -657,7 +661,7 @@ product_kernel(const __grid_constant__ ProductArgs<kProblems> a) {
         Addend d;
         const long long d_at = (t.i * kTile + row) * p.pitch + t.j * kCols;
         if (kCols == 64 && p.out == kOutParts) {
-          finish_staged<kCols>(p, a.m[t.problem], t, at, row, half, alpha, base, smem_u32(&bars->tmem_full[buf]), (n >> 1) & 1u, adds & 1u, bars, a.err);
+          finish_staged<kCols>(p, a.m, t, at, row, half, alpha, base, smem_u32(&bars->tmem_full[buf]), (n >> 1) & 1u, adds & 1u, bars, a.err);
           adds += p.d_hi != nullptr;
           tc_fence_before();
           __syncwarp();
@@ -806,7 +810,7 @@ struct Workspace {
   double* sums;
   float* factors;
   unsigned* arrived;                                 // [kRuns], of the launches with several steps
-  Matrix x[2], g[2], p[2], t, q[2];
+  Matrix all[kMatrices];
 };
 int64_t workspace_of(int m, int k, char* base, Workspace* out) {
   int64_t at = 0;
@@ -827,8 +831,7 @@ int64_t workspace_of(int m, int k, char* base, Workspace* out) {
   w.sums = reinterpret_cast<double*>(take(kNormBlocks * 8));
   w.factors = reinterpret_cast<float*>(take(2 * kRuns * 4));
   w.arrived = reinterpret_cast<unsigned*>(take(kRuns * 4));
-  for (Matrix* x : {&w.x[0], &w.x[1]}) *x = matrix(n, l, ceil_div64(l, 8) * 8);
-  for (Matrix* x : {&w.g[0], &w.g[1], &w.p[0], &w.p[1], &w.t, &w.q[0], &w.q[1]}) *x = matrix(side, side, side);
+  for (int i = 0; i < kMatrices; ++i) w.all[i] = i <= kX1 ? matrix(n, l, ceil_div64(l, 8) * 8) : matrix(side, side, side);
   if (out) *out = w;
   return at;
 }
@@ -843,59 +846,69 @@ rt3d_status launched(cudaError_t e) {
 struct Runner {
   DeviceInfo dev;
   cudaStream_t st;
+  const Workspace& ws;
+  Maps maps[kMatrices];
+  const Matrix& matrix(int id) const { return ws.all[id]; }
 
   static bool map_of(CUtensorMap* map, const __half* p, const Matrix& x, int box_rows) {
     const cuuint64_t dims[2] = {cuuint64_t(x.cols), cuuint64_t(x.rows)}, strides[1] = {cuuint64_t(x.pitch) * 2};
     const cuuint32_t box[2] = {64, cuuint32_t(box_rows)}, estr[2] = {1, 1};
     return encode_tiled(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, const_cast<__half*>(p), dims, strides, box, estr, CU_TENSOR_MAP_SWIZZLE_128B) == CUDA_SUCCESS;
   }
-  static bool maps_of(CUtensorMap (&map)[2], const Matrix& x, int box_rows) { return map_of(&map[0], x.hi, x, box_rows) && map_of(&map[1], x.lo, x, box_rows); }
+  bool make_maps() {
+    for (int i = 0; i < kMatrices; ++i) {
+      const Matrix& x = ws.all[i];
+      for (int q = 0; q < 2; ++q)
+        if (!map_of(&maps[i].rows128[q], q ? x.lo : x.hi, x, kTile) || !map_of(&maps[i].rows64[q], q ? x.lo : x.hi, x, 64)) return false;
+    }
+    return true;
+  }
 
-  // C, where it leaves in tiles of 128 x 64
-  static bool out_maps(Maps* m, const Matrix& c, int cols) { return cols != 64 || maps_of(m->c, c, kTile); }
   // tiles of n x n on and under the diagonal: as wide as 128 rows need, the last row as wide as n
   static int tiles_under(int n, int cols) {
     const int rows = ceil_div(n, kTile), w = kTile / cols;
     return w * (rows - 1) * rows / 2 + (cols == kTile ? rows : ceil_div(n, cols));
   }
   // G = X X^T (of one or two parts)
-  static bool gram(Problem* p, Maps* m, const Matrix& x, int x_parts, const Matrix& g, const float* factor, int cols) {
-    if (!maps_of(m->a, x, kTile) || !maps_of(m->b, x, cols) || !out_maps(m, g, cols)) return false;
+  void gram(Problem* p, int x, int x_parts, int g, const float* factor, int cols) const {
+    p->a = p->b = x; p->c = g;
     p->parts = x_parts == 2 ? 3 : 1; p->same = 1; p->symmetric = 1;
-    p->chunks = ceil_div(x.cols, 64);
-    p->n_tiles = tiles_under(x.rows, cols);
-    p->rows = p->cols = g.rows;
+    p->chunks = ceil_div(matrix(x).cols, 64);
+    p->n_tiles = tiles_under(matrix(x).rows, cols);
     p->factor = factor;
-    p->out = kOutParts; p->alpha = kGScale / (kXScale * kXScale); p->c_hi = g.hi; p->c_lo = g.lo; p->pitch = g.pitch;
-    return true;
+    p->alpha = kGScale / (kXScale * kXScale);
+    out_parts(p, g);
   }
   // C = alpha L R of small symmetric matrices of which n x n exist
-  static bool small(Problem* p, Maps* m, int n, const Matrix& l, const Matrix& r, const Matrix& c, float alpha, int cols) {
-    if (!maps_of(m->a, l, kTile) || !maps_of(m->b, r, cols) || !maps_of(m->a64, l, 64) || !maps_of(m->b64, r, 64) || !out_maps(m, c, cols)) return false;
+  void small(Problem* p, int n, int l, int r, int c, float alpha, int cols) const {
+    p->a = l; p->b = r; p->c = c;
     p->parts = 3; p->symmetric = 1; p->a_under = p->b_under = 1;
     p->chunks = ceil_div(n, 64);
     p->n_tiles = tiles_under(n, cols);
-    p->rows = p->cols = c.rows;
-    p->out = kOutParts; p->alpha = alpha; p->c_hi = c.hi; p->c_lo = c.lo; p->pitch = c.pitch;
-    return true;
+    p->alpha = alpha;
+    out_parts(p, c);
   }
   // P = a + b G + c G G
-  static bool polynomial(Problem* p, Maps* m, int n, const Matrix& g, const Matrix& c, const float* abc, int cols) {
-    if (!small(p, m, n, g, g, c, abc[2] * kPScale / (kGScale * kGScale), cols)) return false;
+  void polynomial(Problem* p, int n, int g, int c, const float* abc, int cols) const {
+    small(p, n, g, g, c, abc[2] * kPScale / (kGScale * kGScale), cols);
     p->same = 1;
     p->beta = abc[1] * kPScale / kGScale; p->diag = abc[0] * kPScale;
-    p->d_hi = g.hi; p->d_lo = g.lo;
-    return true;
+    p->d_hi = matrix(g).hi; p->d_lo = matrix(g).lo;
   }
-  // C = alpha Q X
-  static bool apply(Problem* p, Maps* m, const Matrix& q, const Matrix& x, int x_parts, const float* factor, int cols) {
-    if (!maps_of(m->a, q, kTile) || !maps_of(m->a64, q, 64) || !maps_of(m->b64, x, 64)) return false;
+  // alpha Q X; where it goes is the caller's to say
+  void apply(Problem* p, int q, int x_id, int x_parts, const float* factor, int cols) const {
+    const Matrix& x = matrix(x_id);
+    p->a = q; p->b = x_id; p->c = -1;
     p->parts = x_parts == 2 ? 3 : 2; p->a_under = 1; p->b_rows = 1;
     p->chunks = ceil_div(x.rows, 64);
     p->tiles_m = ceil_div(x.rows, kTile); p->n_tiles = p->tiles_m * ceil_div(x.cols, cols);
     p->rows = x.rows; p->cols = x.cols;
     p->factor = factor; p->alpha = 1.f / kPScale;
-    return true;
+  }
+  void out_parts(Problem* p, int c, int parts = 2) const {
+    const Matrix& m = matrix(c);
+    p->out = kOutParts; p->c = c; p->c_hi = m.hi; p->c_lo = parts == 2 ? m.lo : nullptr; p->pitch = m.pitch;
+    p->rows = m.rows; p->cols = m.cols;
   }
 
   template <int kCols, int kProblems>
@@ -909,6 +922,7 @@ struct Runner {
       attr_done[d].store(true);
     }
     a.err = dev.err;
+    std::memcpy(a.m, maps, sizeof(maps));
     LaunchSetup ls(dim3(unsigned(grid)), dim3(kProductThreads), kProductSmem<kCols>, st, cluster);
     if (cooperative) {
       ls.attr[0].id = cudaLaunchAttributeCooperative;
@@ -938,6 +952,7 @@ struct Fused {
     std::memset(&a, 0, sizeof(a));
     n_problems = 0;
   }
+  Problem* add() { return &a.steps.p[n_problems++]; }
   void end_step() { a.steps.first[++a.n_steps] = n_problems; }
   // A cluster's wait takes 0.5 us, a grid's 1.5: eight CTAs where going round more often than a grid would costs less than that
   // (a chunk of three products of 128 x 64: 700 clocks).
@@ -987,7 +1002,8 @@ int later_parts(const Plan& plan, int done) {
 template <typename T>
 rt3d_status direction(const Source<T>& src, int m, int k, const Plan& plan, int first, bool exact, const Workspace& ws, const Result& res,
                       const DeviceInfo& dev, cudaStream_t st) {
-  const Runner r{dev, st};
+  Runner r{dev, st, ws};
+  if (!r.make_maps()) return RT3D_ERR_CUDA;
   const bool turned = m > k;
   const bool short_x = (turned ? k : m) <= kFusedSide && (turned ? m : k) <= kFusedLength;
   uintptr_t bits = reinterpret_cast<uintptr_t>(src.g) | uintptr_t(src.pitch) * sizeof(T);       // 4 values at a time
@@ -997,7 +1013,7 @@ rt3d_status direction(const Source<T>& src, int m, int k, const Plan& plan, int 
   rt3d_status s = launched(vec ? cudaLaunchKernelEx(&l1.cfg, square_sums_kernel<T, true>, src, m, k, ws.sums)
                                : cudaLaunchKernelEx(&l1.cfg, square_sums_kernel<T, false>, src, m, k, ws.sums));
   if (s != RT3D_OK) return s;
-  const Matrix *x = &ws.x[0], *next = &ws.x[1];
+  const Matrix* x = &ws.all[kX0];
   int parts = !exact && sizeof(T) == 2 ? 1 : 2;
   __half* lo = parts == 2 ? x->lo : nullptr;
   int runs = 0;
@@ -1021,71 +1037,63 @@ rt3d_status direction(const Source<T>& src, int m, int k, const Plan& plan, int 
     chain.reset();
     return e;
   };
-  const Matrix *cur = x, *other = next;
+  int cur = kX0, other = kX1;
   for (int done = 0, run = 0; done < plan.steps; ++run) {
     const int steps = run_steps(plan, done, short_x ? 1 : run ? 3 : first);
-    const Matrix *g = &ws.g[0], *g2 = &ws.g[1], *p = &ws.p[0], *p2 = &ws.p[1], *q = nullptr;
+    int g = kG0, g2 = kG1, p = kP0, p2 = kP1, q = -1, q_next = kQ0;
     const int cols = n_fused ? 64 : kTile;
-    int q_next = 0;
     if (short_x) {
       if (chain.n_problems + 3 > kMostProblems && (s = flush()) != RT3D_OK) return s;
-      const int at = chain.n_problems++;
-      if (!Runner::gram(&chain.a.steps.p[at], &chain.a.m[at], *cur, parts, *g, ws.factors + run, cols)) return RT3D_ERR_CUDA;
+      r.gram(chain.add(), cur, parts, g, ws.factors + run, cols);
       chain.end_step();
     } else {
       std::memset(&one, 0, sizeof(one));
-      if (!Runner::gram(&one.steps.p[0], &one.m[0], *cur, parts, *g, ws.factors + run, kTile)) return RT3D_ERR_CUDA;
+      r.gram(&one.steps.p[0], cur, parts, g, ws.factors + run, kTile);
       if ((s = r.run(one, 1)) != RT3D_OK) return s;
     }
     // a step of one or two products
     auto products = [&](auto&& first_product, auto&& second_product, int count) -> rt3d_status {
       if (!n_fused) std::memset(&one, 0, sizeof(one));
-      for (int i = 0; i < count; ++i) {
-        const int at = n_fused ? chain.n_problems++ : i;
-        Problem* p = n_fused ? &chain.a.steps.p[at] : &one.steps.p[at];
-        Maps* m = n_fused ? &chain.a.m[at] : &one.m[at];
-        if (!(i ? second_product(p, m) : first_product(p, m))) return RT3D_ERR_CUDA;
-      }
+      first_product(n_fused ? chain.add() : &one.steps.p[0]);
+      if (count == 2) second_product(n_fused ? chain.add() : &one.steps.p[1]);
       if (!n_fused) return r.run(one, count);
       chain.end_step();
       return RT3D_OK;
     };
     for (int i = 0; i < steps; ++i) {
-      const bool more = i + 1 < steps;
-      auto make_p = [&](Problem* to, Maps* maps) { return Runner::polynomial(to, maps, n, *g, *p, plan.abc[done + i], cols); };
-      auto make_t = [&](Problem* to, Maps* maps) { return Runner::small(to, maps, n, *p, *g, ws.t, kGScale / (kPScale * kGScale), cols); };           // T = P G
-      auto make_q = [&](Problem* to, Maps* maps) { return Runner::small(to, maps, n, *p, *q, ws.q[q_next], 1.f / kPScale, cols); };                   // Q = P Q
-      auto make_g = [&](Problem* to, Maps* maps) { return Runner::small(to, maps, n, ws.t, *p, *g2, 1.f / kPScale, cols); };                          // G = T P
+      const bool more = i + 1 < steps, has_q = q >= 0;
+      auto make_p = [&](Problem* to) { r.polynomial(to, n, g, p, plan.abc[done + i], cols); };
+      auto make_t = [&](Problem* to) { r.small(to, n, p, g, kT, kGScale / (kPScale * kGScale), cols); };         // T = P G
+      auto make_q = [&](Problem* to) { r.small(to, n, p, q, q_next, 1.f / kPScale, cols); };                     // Q = P Q
+      auto make_g = [&](Problem* to) { r.small(to, n, kT, p, g2, 1.f / kPScale, cols); };                        // G = T P
       if ((s = products(make_p, make_p, 1)) != RT3D_OK) return s;
-      if (more || q) {
-        s = more && q ? products(make_t, make_q, 2) : more ? products(make_t, make_t, 1) : products(make_q, make_q, 1);
+      if (more || has_q) {
+        s = more && has_q ? products(make_t, make_q, 2) : more ? products(make_t, make_t, 1) : products(make_q, make_q, 1);
         if (s != RT3D_OK) return s;
       }
-      if (q) {
-        q = &ws.q[q_next];
-        q_next ^= 1;
+      if (has_q) {
+        q = q_next;
+        q_next = q_next == kQ0 ? kQ1 : kQ0;
       }
       if (more) {
         if ((s = products(make_g, make_g, 1)) != RT3D_OK) return s;
-        const Matrix* was = g; g = g2; g2 = was;
+        const int was = g; g = g2; g2 = was;
       }
-      if (!q) { q = p; const Matrix* was = p; p = p2; p2 = was; }                                       // the first P is the first Q
+      if (!has_q) { q = p; const int was = p; p = p2; p2 = was; }                                                // the first P is the first Q
     }
     done += steps;
     const bool last = done == plan.steps;
-    Problem* c = short_x ? &chain.a.steps.p[chain.n_problems] : &one.steps.p[0];
-    Maps* c_maps = short_x ? &chain.a.m[chain.n_problems++] : &one.m[0];
     if (!short_x) {
       if ((s = flush()) != RT3D_OK) return s;
       std::memset(&one, 0, sizeof(one));
     }
-    if (!Runner::apply(c, c_maps, *q, *cur, parts, ws.factors + kRuns + run, short_x ? cols : kTile)) return RT3D_ERR_CUDA;
+    Problem* c = short_x ? chain.add() : &one.steps.p[0];
+    r.apply(c, q, cur, parts, ws.factors + kRuns + run, short_x ? cols : kTile);
     if (last) {
       c->out = res.out; c->alpha /= kXScale;
     } else {
-      if (!Runner::out_maps(c_maps, *other, short_x ? cols : kTile)) return RT3D_ERR_CUDA;
       parts = exact ? 2 : later_parts(plan, done);
-      c->out = kOutParts; c->c_hi = other->hi; c->c_lo = parts == 2 ? other->lo : nullptr; c->pitch = other->pitch;
+      r.out_parts(c, other, parts);
     }
     auto results = [&](auto& args) {
       args.turned = res.turned; args.bf = res.bf; args.w = res.w; args.mask = res.mask;
@@ -1099,7 +1107,7 @@ rt3d_status direction(const Source<T>& src, int m, int k, const Plan& plan, int 
       results(one);
       if ((s = r.run(one, 1)) != RT3D_OK) return s;
     }
-    const Matrix* was = cur; cur = other; other = was;
+    const int was = cur; cur = other; other = was;
   }
   return RT3D_OK;
 }

@@ -452,40 +452,35 @@ __device__ __forceinline__ void finish_staged(const Problem& p, const Maps* maps
   epilogue_bar_sync(256);                            // the leader has waited for the last tile's way out
   if (add) ok = mbar_wait_warp(d_bar, d_parity, bars, err, 6) && ok;
   if (ok) {
+    const uint32_t line = out + row * 128;
+    const int diagonal = p.symmetric ? t.i * kTile + row - t.j * kCols - half * 32 : -1;        // of this row's columns
+    uint32_t r[32];
+    __syncwarp();
+    tmem_ld32(taddr + half * 32, r);
 #pragma unroll
-    for (int q = 0; q < 2; ++q) {
-      const int c0 = half * 32 + q * 16;
-      uint32_t r[16];
-      __syncwarp();
-      tmem_ld16(taddr + c0, r);
-      float v[16];
+    for (int u = 0; u < 4; ++u) {
+      const uint32_t at = line + (((half * 4 + u) ^ (row & 7)) << 4);
+      float v[8];
 #pragma unroll
-      for (int e = 0; e < 16; ++e) v[e] = alpha * __uint_as_float(r[e]);
-      const uint32_t line = out + row * 128;
+      for (int e = 0; e < 8; ++e) v[e] = alpha * __uint_as_float(r[8 * u + e]);
+      if (add) {
+        const uint4 dh = lds128(at), dl = lds128(at + kRowsBytes);
+        const __half2 *hh = reinterpret_cast<const __half2*>(&dh), *ll = reinterpret_cast<const __half2*>(&dl);
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        const uint32_t at = line + (((c0 / 8 + u) ^ (row & 7)) << 4);
-        if (add) {
-          const uint4 dh = lds128(at), dl = lds128(at + kRowsBytes);
-          const __half2 *hh = reinterpret_cast<const __half2*>(&dh), *ll = reinterpret_cast<const __half2*>(&dl);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const float2 x = __half22float2(hh[e]), y = __half22float2(ll[e]);
-            v[8 * u + 2 * e] += p.beta * (x.x + y.x); v[8 * u + 2 * e + 1] += p.beta * (x.y + y.y);
-          }
+        for (int e = 0; e < 4; ++e) {
+          const float2 x = __half22float2(hh[e]), y = __half22float2(ll[e]);
+          v[2 * e] += p.beta * (x.x + y.x); v[2 * e + 1] += p.beta * (x.y + y.y);
         }
-        if (p.symmetric) {
-          const int i = t.i * kTile + row, j = t.j * kCols + c0 + 8 * u;
+        if ((diagonal >> 3) == u) {
 #pragma unroll
-          for (int e = 0; e < 8; ++e)
-            if (i == j + e) v[8 * u + e] += p.diag;
+          for (int e = 0; e < 8; ++e) v[e] += (diagonal & 7) == e ? p.diag : 0.f;
         }
-        __half2 h[4], l[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) split_half2(v[8 * u + 2 * e], v[8 * u + 2 * e + 1], h[e], l[e]);
-        sts128(at, *reinterpret_cast<const uint4*>(h));
-        sts128(at + kRowsBytes, *reinterpret_cast<const uint4*>(l));
       }
+      __half2 h[4], l[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) split_half2(v[2 * e], v[2 * e + 1], h[e], l[e]);
+      sts128(at, *reinterpret_cast<const uint4*>(h));
+      sts128(at + kRowsBytes, *reinterpret_cast<const uint4*>(l));
     }
   }
   asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -571,51 +566,59 @@ product_kernel(const __grid_constant__ ProductArgs<kProblems> a) {
   for (int s = 0; s < a.n_steps; ++s) {
     int n_items = 0;
     for (int p = steps.first[s]; p < steps.first[s + 1]; ++p) n_items += steps.p[p].n_tiles;
+    TileAt t0{0, 0, 0};                              // this CTA's first, found while the others end the last step
+    if (cta < n_items) t0 = tile_at<kCols>(steps, s, cta);
+    if (kProblems > 1 && s > 0) {
+      // What the last step has written is what this one's copies read: both through the same proxy, so that once the stores are
+      // complete (which this waits for) the barrier orders the two.
+      if (threadIdx.x == 64) tma_store_wait_all();
+      if (a.one_cluster) {                           // a release and an acquire of the cluster
+        __syncwarp();
+        cluster_sync_all();
+      } else {
+        grid_barrier(a.arrived, unsigned(s) * gridDim.x, bars, a.err);
+        if (bars->abort_flag) break;                 // this CTA's steps end here; the others' waits run out
+      }
+    }
     if (warp == 0) {
       // ---------------------------------------------------------------- loads
-      if (lane == 0) {
-        bool ok = true;
-        for (int item = cta; item < n_items && ok; item += n_ctas) {
-          const TileAt t = tile_at<kCols>(steps, s, item);
-          const Problem& p = steps.p[t.problem];
-          const Maps &ma = a.m[p.a], &mb = a.m[p.b];
-          const CUtensorMap* b_maps = kCols == 64 ? mb.rows64 : mb.rows128;
-          const bool one = kCols == kTile && p.same && t.i == t.j;
-          const int a_parts = p.parts >= 2 ? 2 : 1, b_parts = one ? 0 : p.parts == 3 ? 2 : 1;
-          const int c_last = p.chunks * (split + 1) / a.splits;
-          for (int c = p.chunks * split / a.splits; c < c_last; ++c) {
-            const uint32_t full = smem_u32(&bars->full[stage]), at = base + stage * S::kBytes;
-            if (!mbar_wait(smem_u32(&bars->empty[stage]), phase ^ 1u, bars, a.err, 1)) { ok = false; break; }
-            mbar_expect_tx(full, uint32_t(a_parts) * kRowsBytes + uint32_t(b_parts) * S::kColsBytes);
-            const bool a_turned = above(p.a_under, c, t.i * kTile), b_turned = p.b_rows || above(p.b_under, c, t.j * kCols);
-            for (int q = 0; q < a_parts; ++q) {
-              const uint32_t to = at + q * kRowsBytes;
-              if (a_turned) {
-                tma_load_2d(to, &ma.rows64[q], full, t.i * kTile, c * 64);
-                tma_load_2d(to + 8192, &ma.rows64[q], full, t.i * kTile + 64, c * 64);
-              } else {
-                tma_load_2d(to, &ma.rows128[q], full, c * 64, t.i * kTile);
-              }
-            }
-            for (int q = 0; q < b_parts; ++q) {
-              const uint32_t to = at + S::kBAt + q * S::kColsBytes;
-              if (b_turned) {
-#pragma unroll
-                for (int h = 0; h < kCols / 64; ++h) tma_load_2d(to + h * 8192, &mb.rows64[q], full, t.j * kCols + 64 * h, c * 64);
-              } else {
-                tma_load_2d(to, &b_maps[q], full, c * 64, t.j * kCols);
-              }
-            }
-            if (++stage == S::kRing) { stage = 0; phase ^= 1u; }
+      // Lanes 0 to 3 copy A hi, A lo, B hi and B lo, lanes 4 to 7 the second 64 columns of those that come as transposes: a copy's
+      // address, descriptor and coordinates are 200 clocks of one thread's time.
+      const int q = lane & 1, h = lane >> 2;
+      const bool of_b = lane & 2;
+      bool ok = true;
+      for (int item = cta; item < n_items && ok; item += n_ctas) {
+        const TileAt t = item == cta ? t0 : tile_at<kCols>(steps, s, item);
+        const Problem& p = steps.p[t.problem];
+        const bool one = kCols == kTile && p.same && t.i == t.j;
+        const int a_parts = p.parts >= 2 ? 2 : 1, b_parts = one ? 0 : p.parts == 3 ? 2 : 1;
+        const uint32_t bytes = uint32_t(a_parts) * kRowsBytes + uint32_t(b_parts) * S::kColsBytes;
+        const Maps& m = a.m[of_b ? p.b : p.a];
+        const CUtensorMap *straight = of_b && kCols == 64 ? &m.rows64[q] : &m.rows128[q], *turned = &m.rows64[q];
+        const uint32_t to = base + (of_b ? S::kBAt + q * S::kColsBytes : q * kRowsBytes);
+        const int at = of_b ? t.j * kCols : t.i * kTile, under = of_b ? p.b_under : p.a_under;
+        const bool always = of_b && p.b_rows, mine = lane < 8 && q < (of_b ? b_parts : a_parts), wide = !of_b || kCols == kTile;
+        const int c_last = p.chunks * (split + 1) / a.splits;
+        for (int c = p.chunks * split / a.splits; c < c_last; ++c) {
+          const uint32_t full = smem_u32(&bars->full[stage]);
+          const bool is_turned = always || above(under, c, at);
+          if (!mbar_wait_warp(smem_u32(&bars->empty[stage]), phase ^ 1u, bars, a.err, 1)) { ok = false; break; }
+          if (lane == 0) mbar_expect_tx(full, bytes);
+          __syncwarp();
+          if (mine && h <= (is_turned && wide ? 1 : 0)) {
+            if (is_turned) tma_load_2d(to + stage * S::kBytes + h * 8192, turned, full, at + 64 * h, c * 64);
+            else tma_load_2d(to + stage * S::kBytes, straight, full, c * 64, at);
           }
+          if (++stage == S::kRing) { stage = 0; phase ^= 1u; }
         }
       }
+      __syncwarp();
     } else if (warp == 1) {
       // ---------------------------------------------------------------- products
       const bool elected = elect_one();
       bool ok = true;
       for (int item = cta; item < n_items && ok; item += n_ctas, ++n) {
-        const TileAt t = tile_at<kCols>(steps, s, item);
+        const TileAt t = item == cta ? t0 : tile_at<kCols>(steps, s, item);
         const Problem& p = steps.p[t.problem];
         const bool one = kCols == kTile && p.same && t.i == t.j;
         const uint32_t buf = n & 1u, d = tmem + buf * kCols;
@@ -654,7 +657,7 @@ product_kernel(const __grid_constant__ ProductArgs<kProblems> a) {
       // ---------------------------------------------------------------- results
       const int quad = warp & 3, half = (warp - 2) >> 2, row = quad * 32 + lane;
       for (int item = cta; item < n_items; item += n_ctas, ++n) {
-        const TileAt t = tile_at<kCols>(steps, s, item);
+        const TileAt t = item == cta ? t0 : tile_at<kCols>(steps, s, item);
         const Problem& p = steps.p[t.problem];
         const float alpha = p.factor ? p.alpha * __ldcg(p.factor) : p.alpha;
         const uint32_t buf = n & 1u, at = tmem + (uint32_t(quad * 32) << 16) + buf * kCols;
@@ -713,20 +716,6 @@ product_kernel(const __grid_constant__ ProductArgs<kProblems> a) {
             }
           }
         }
-      }
-    }
-    if (kProblems > 1 && s + 1 < a.n_steps) {
-      // What this step has written is what the next one's copies read: both through the same proxy, so that once the stores are
-      // complete (which this waits for) the barrier orders the two.
-      if (threadIdx.x == 64) tma_store_wait_all();
-      if (a.one_cluster) {                           // a release and an acquire of the cluster
-        __syncwarp();
-        cluster_sync_all();
-      } else {
-        grid_barrier(a.arrived, unsigned(s + 1) * gridDim.x, bars, a.err);
-      }
-      if (bars->abort_flag) {                        // this CTA's steps end here; the others' waits run out
-        if (!a.one_cluster) break;
       }
     }
   }

@@ -9,6 +9,7 @@
 #include "rt3d.h"
 #include "rt3d_internal.h"
 #include "umma_common.cuh"
+#include "w4.cuh"
 
 namespace rt3d {
 namespace {
@@ -18,17 +19,9 @@ __device__ __forceinline__ uint32_t cluster_size() {
   asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(r));
   return r;
 }
-__device__ __forceinline__ float ld_cluster_f32(uint32_t addr) {
-  float v;
-  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
-  return v;
-}
-// max(v, 0) that lets a NaN through.
-__device__ __forceinline__ float relu_of(float v) { return v < 0.f ? 0.f : v; }
 
 __device__ __forceinline__ void store_value(float* p, float v) { *p = v; }
 __device__ __forceinline__ void store_value(__nv_bfloat16* p, float v) { *p = __float2bfloat16_rn(v); }
-__device__ __forceinline__ float bf16_float(uint16_t b) { return __uint_as_float(uint32_t(b) << 16); }
 
 __device__ __forceinline__ int shift_of(int e) { return 4 * ((e >> 1) + 4 * (e & 1)); }
 
@@ -268,24 +261,9 @@ w4_unpack_kernel(T* __restrict__ w, const GridArgs a) {
 // A CTA's eight warps take every eighth block of 64 inputs of kTiles tiles of filters; where there are few tiles, the CTAs of a cluster
 // share the inputs further and add their sums up through one another's shared memory, always in the same order.
 constexpr int kLinearThreads = 256;
+constexpr int kMostRows = 1 << 19;                          // of a launch
+constexpr int kManyRows = 32;                               // more bf16 rows go to linear_w4_many_rows
 
-__device__ __forceinline__ uint32_t fma_bf16x2(uint32_t a, uint32_t b, uint32_t c) {
-  uint32_t d;
-  asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(d) : "r"(a), "r"(b), "r"(c));
-  return d;
-}
-constexpr uint32_t kTwo127 = 0x7f007f00u, kTwo123 = 0x7d007d00u;               // bf16 2^127 and 2^123, twice
-constexpr uint32_t kMinusEighth = 0xbe00be00u;                                 // -8 / 64, twice
-// -z / 64, twice: 128 + z has z in its mantissa, and -(128 + z) / 64 + 2.
-__device__ __forceinline__ uint32_t minus_zero(uint32_t z) { return fma_bf16x2(z * 0x00010001u + 0x43004300u, 0xbc80bc80u, 0x40004000u); }
-// Eight codes of a word as four pairs of (code - zero) / 64, inputs (2 p, 2 p + 1).
-__device__ __forceinline__ void spread_codes(uint32_t w, uint32_t minus, uint32_t (&v)[4]) {
-  const uint32_t u = w >> 8;
-  v[0] = fma_bf16x2(w & 0x000F000Fu, kTwo127, minus);
-  v[1] = fma_bf16x2(w & 0x00F000F0u, kTwo123, minus);
-  v[2] = fma_bf16x2(u & 0x000F000Fu, kTwo127, minus);
-  v[3] = fma_bf16x2(u & 0x00F000F0u, kTwo123, minus);
-}
 __device__ __forceinline__ void mma_bf16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
   asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
       : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
@@ -340,17 +318,6 @@ struct Operand<float> {
   }
 };
 
-struct LinearArgs {
-  const uint4* codes;
-  const uint16_t* scales;
-  const uint8_t* zeros;
-  const float* bias;
-  const void* x;
-  void* y;
-  long long x_pitch, y_pitch;
-  int m, k, group_shift, n_groups, k_blocks, n_tiles, relu;
-  int rows;
-};
 
 // A stage of a warp's ring: kDeep neighbouring blocks of 64 inputs: the codes [block][tile], the rows of x [block], then the
 // groups' scales [tile][group] and zero points.
@@ -699,13 +666,25 @@ rt3d_status launch_linear(const LinearArgs& a, bool fine, int ctas, int ranks, c
   return launched(cudaLaunchKernelEx(&ls.cfg, kernel, a));
 }
 template <typename T>
-rt3d_status linear(const rt3d_tensor* x, const rt3d_w4* q, const float* bias, int relu, rt3d_tensor* y, long long rows, int sms, cudaStream_t st) {
+rt3d_status linear(const rt3d_tensor* x, const rt3d_w4* q, const float* bias, int relu, rt3d_tensor* y, long long rows, const DeviceInfo& dev, cudaStream_t st) {
+  const int sms = dev.sm_count;
   LinearArgs a;
   a.codes = reinterpret_cast<const uint4*>(q->codes);
   a.scales = q->scales; a.zeros = q->zeros; a.bias = bias; a.x = x->data; a.y = y->data;
   a.x_pitch = x->c_stride; a.y_pitch = y->c_stride;
-  a.m = q->m; a.k = q->k; a.group_shift = q->group == 128 ? 1 : 0; a.n_groups = ceil_div(q->k, q->group);
+  a.m = q->m; a.k = q->k; a.group_shift = q->group == 128 ? 1 : 0; a.fine = q->group == 32 ? 1 : 0; a.n_groups = ceil_div(q->k, q->group);
   a.k_blocks = ceil_div(q->k, 64); a.n_tiles = ceil_div(q->m, 16); a.relu = relu ? 1 : 0; a.rows = int(rows);
+  if (rows > kMostRows) {                                     // the grid's second extent: one launch after another
+    for (long long r = 0; r < rows; r += kMostRows) {
+      rt3d_tensor xs = *x, ys = *y;
+      xs.data = static_cast<T*>(x->data) + r * x->c_stride;
+      ys.data = static_cast<T*>(y->data) + r * y->c_stride;
+      const rt3d_status s = linear<T>(&xs, q, bias, relu, &ys, rows - r < kMostRows ? rows - r : kMostRows, dev, st);
+      if (s != RT3D_OK) return s;
+    }
+    return RT3D_OK;
+  }
+  if (sizeof(T) == 2 && rows > kManyRows) return linear_w4_many_rows(a, dev, st);
   // fp32 rows take three times the registers: 16 at a time at most, in two tiles
   constexpr bool kWide = sizeof(T) == 2;
   const int rows8 = rows <= 8 ? 1 : rows <= 16 || !kWide ? 2 : 4;
@@ -779,8 +758,8 @@ rt3d_status rt3d_linear_w4(const rt3d_tensor* x, const rt3d_w4* q, const float* 
   if ((s = current_device_info(&dev)) != RT3D_OK) return s;
   if (dev.cc_major != 10) return RT3D_ERR_UNSUPPORTED;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  return x->dtype == RT3D_BF16 ? linear<__nv_bfloat16>(x, q, bias, relu, y, rows, dev.sm_count, st)
-                               : linear<float>(x, q, bias, relu, y, rows, dev.sm_count, st);
+  return x->dtype == RT3D_BF16 ? linear<__nv_bfloat16>(x, q, bias, relu, y, rows, dev, st)
+                               : linear<float>(x, q, bias, relu, y, rows, dev, st);
 }
 
 }  // extern "C"

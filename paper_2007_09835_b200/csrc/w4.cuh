@@ -1,0 +1,58 @@
+// What the kernels of products with 4-bit weights share.  Included by .cu files only, after umma_common.cuh.
+#pragma once
+
+#include <cuda_runtime.h>
+
+#include <cstdint>
+
+#include "rt3d.h"
+#include "rt3d_internal.h"
+
+namespace rt3d {
+
+struct LinearArgs {
+  const uint4* codes;
+  const uint16_t* scales;
+  const uint8_t* zeros;
+  const float* bias;
+  const void* x;
+  void* y;
+  long long x_pitch, y_pitch;
+  int m, k, group_shift, fine, n_groups, k_blocks, n_tiles, relu;
+  int rows;
+};
+
+// Many bf16 rows (w4_umma.cu), at most 2^22.
+rt3d_status linear_w4_many_rows(const LinearArgs& a, const DeviceInfo& dev, cudaStream_t st);
+
+namespace {
+
+__device__ __forceinline__ float bf16_float(uint16_t b) { return __uint_as_float(uint32_t(b) << 16); }
+// max(v, 0) that lets a NaN through.
+__device__ __forceinline__ float relu_of(float v) { return v < 0.f ? 0.f : v; }
+__device__ __forceinline__ float ld_cluster_f32(uint32_t addr) {
+  float v;
+  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
+  return v;
+}
+
+__device__ __forceinline__ uint32_t fma_bf16x2(uint32_t a, uint32_t b, uint32_t c) {
+  uint32_t d;
+  asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(d) : "r"(a), "r"(b), "r"(c));
+  return d;
+}
+constexpr uint32_t kTwo127 = 0x7f007f00u, kTwo123 = 0x7d007d00u;               // bf16 2^127 and 2^123, twice
+constexpr uint32_t kMinusEighth = 0xbe00be00u;                                 // -8 / 64, twice
+// -z / 64, twice: 128 + z has z in its mantissa, and -(128 + z) / 64 + 2.
+__device__ __forceinline__ uint32_t minus_zero(uint32_t z) { return fma_bf16x2(z * 0x00010001u + 0x43004300u, 0xbc80bc80u, 0x40004000u); }
+// Eight codes of a word as four pairs of (code - zero) / 64, inputs (2 p, 2 p + 1).
+__device__ __forceinline__ void spread_codes(uint32_t w, uint32_t minus, uint32_t (&v)[4]) {
+  const uint32_t u = w >> 8;
+  v[0] = fma_bf16x2(w & 0x000F000Fu, kTwo127, minus);
+  v[1] = fma_bf16x2(w & 0x00F000F0u, kTwo123, minus);
+  v[2] = fma_bf16x2(u & 0x000F000Fu, kTwo127, minus);
+  v[3] = fma_bf16x2(u & 0x00F000F0u, kTwo123, minus);
+}
+
+}  // namespace
+}  // namespace rt3d

@@ -1,0 +1,301 @@
+// Products of many bf16 rows with 4-bit weights, on tcgen05.
+//
+// As in w4.cu a group's sum of (c - z) x is exact but for the fp32 additions, and its scale multiplies it in fp32: so every group has
+// an accumulator of its own in tensor memory, which the warps for the results drain into registers, times the scale of their filter,
+// while the next groups' products run.  128 filters are the products' rows (TMEM lanes: a thread has one filter, whose scale is
+// one number), kCols rows of x their columns.  Eight warps turn codes into the bf16 operand (c - z) / 64 in shared memory, 128 filters x
+// 64 inputs a stage; x comes by TMA, which also makes zeros of what lies behind the last input and row.
+// Bound by shared memory: a stage of 128 filters x 64 inputs x 128 rows writes 32 KB and reads 32 KB, 512 clocks at 128 bytes a clock,
+// against 256 of the tensor cores.
+#include <cuda.h>
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+
+#include <atomic>
+#include <cstdint>
+#include <cstring>
+
+#include "pdl.cuh"
+#include "rt3d.h"
+#include "rt3d_internal.h"
+#include "umma_common.cuh"
+#include "w4.cuh"
+
+namespace rt3d {
+
+CUresult encode_tiled(CUtensorMap* map, CUtensorMapDataType type, cuuint32_t rank, void* data, const cuuint64_t* dims, const cuuint64_t* strides,
+                      const cuuint32_t* box, const cuuint32_t* steps, CUtensorMapSwizzle swizzle);      // api.cu
+
+namespace {
+
+constexpr int kResultWarps = 8, kCodeWarps = 8, kThreads = 32 * (2 + kResultWarps + kCodeWarps);
+constexpr int kSums = 4;                             // accumulators in tensor memory
+constexpr uint32_t kFilterBytes = 128 * 128;         // 128 filters x 64 bf16
+constexpr int kAhead = 4;                            // blocks of codes on their way to a warp
+
+struct ManyBars {
+  Barriers b;                                        // full, empty: the ring
+  unsigned long long sum_full[kSums], sum_empty[kSums];
+};
+
+template <int kCols>
+struct ManyShape {
+  static constexpr uint32_t kStage = kFilterBytes + kCols * 128;
+  static constexpr int kRing = kCols == 64 ? 8 : 6;
+  static constexpr uint32_t kPart = 128 * kCols * 4, kBytes = kRing * kStage + 1024 + sizeof(ManyBars);
+  static_assert(kPart <= kRing * kStage, "the sums go where the ring was");
+};
+
+template <int kCols, bool kZeros>
+__global__ void __launch_bounds__(kThreads, 1)
+linear_w4_many_kernel(const __grid_constant__ CUtensorMap xmap, const LinearArgs a, int splits, int32_t* __restrict__ err) {
+  typedef ManyShape<kCols> S;
+  extern __shared__ unsigned char smem_raw[];
+  const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+  unsigned char* ring = smem_raw + (base - smem_u32(smem_raw));
+  ManyBars* mb = reinterpret_cast<ManyBars*>(ring + S::kRing * S::kStage);
+  Barriers* bars = &mb->b;
+  const int warp = uniform(int(threadIdx.x >> 5)), lane = threadIdx.x & 31;
+  const int split = splits > 1 ? int(cluster_ctarank()) : 0;
+  const int filter0 = int(blockIdx.x) / splits * 128;
+  const long long row0 = (long long)blockIdx.y * kCols;
+  // blocks of 64 inputs, in pairs so that no group is cut
+  const int pairs = (a.k_blocks + 1) / 2;
+  const int b_first = 2 * int((long long)pairs * split / splits), b_last = min(2 * int((long long)pairs * (split + 1) / splits), a.k_blocks);
+  // 16s of inputs in a group: 2, 4 or 8
+  const int shift = a.group_shift + 2 - (a.fine ? 1 : 0), per_group = 1 << shift;
+  const int n_sums = ((b_last - b_first) * 4 + per_group - 1) >> shift;
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < S::kRing; ++s) { mbar_init(smem_u32(&bars->full[s]), 1 + kCodeWarps); mbar_init(smem_u32(&bars->empty[s]), 1); }
+    for (int q = 0; q < kSums; ++q) { mbar_init(smem_u32(&mb->sum_full[q]), 1); mbar_init(smem_u32(&mb->sum_empty[q]), kResultWarps); }
+    bars->abort_flag = 0;
+    bars->wait_limit = kWaitCycles;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    tma_prefetch_map(&xmap);
+  }
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;"
+                 ::"r"(smem_u32(&bars->tmem_base)), "r"(uint32_t(kSums * kCols)) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = uniform(uint32_t(bars->tmem_base));
+  pdl_launch();
+  pdl_wait();
+
+  if (warp == 0) {
+    // ------------------------------------------------------------------ rows of x
+    if (lane == 0) {
+      int stage = 0;
+      uint32_t phase = 0;
+      for (int b = b_first; b < b_last; ++b) {
+        const uint32_t full = smem_u32(&bars->full[stage]);
+        if (!mbar_wait(smem_u32(&bars->empty[stage]), phase ^ 1u, bars, err, 1)) break;
+        mbar_expect_tx(full, uint32_t(kCols) * 128);
+        tma_load_2d(base + stage * S::kStage + kFilterBytes, &xmap, full, b * 64, int(row0));
+        if (++stage == S::kRing) { stage = 0; phase ^= 1u; }
+      }
+    }
+  } else if (warp == 1) {
+    // ------------------------------------------------------------------ products
+    const bool elected = elect_one();
+    const uint32_t idesc = instr_desc_bf16(kCols);
+    int stage = 0, sum = 0;
+    uint32_t phase = 0;
+    bool ok = true;
+    for (int b = b_first; b < b_last && ok; ++b) {
+      if (!mbar_wait_warp(smem_u32(&bars->full[stage]), phase, bars, err, 2)) break;
+      tc_fence_after();
+      const uint32_t at = base + stage * S::kStage;
+      const uint64_t filters = smem_desc_sw128(at), rows = smem_desc_sw128(at + kFilterBytes);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int in = ((b - b_first) * 4 + k) & (per_group - 1);            // place in its group
+        const int buf = sum % kSums;
+        if (in == 0) {
+          if (!mbar_wait_warp(smem_u32(&mb->sum_empty[buf]), (uint32_t(sum / kSums) & 1u) ^ 1u, bars, err, 3)) { ok = false; break; }
+          tc_fence_after();
+        }
+        if (elected) umma_bf16(tmem + buf * kCols, filters + 2 * k, rows + 2 * k, idesc, in ? 1u : 0u);
+        if (in == per_group - 1 || (k == 3 && b + 1 == b_last)) {
+          if (elected) umma_commit(smem_u32(&mb->sum_full[buf]));
+          ++sum;
+        }
+      }
+      if (ok && elected) umma_commit(smem_u32(&bars->empty[stage]));
+      if (++stage == S::kRing) { stage = 0; phase ^= 1u; }
+    }
+    __syncwarp();
+  } else if (warp < 2 + kResultWarps) {
+    // ------------------------------------------------------------------ results
+    constexpr int kMine = kCols / 2;                 // columns of this thread
+    const int quad = warp & 3, half = (warp - 2) >> 2, filter = quad * 32 + lane;
+    const int tile = min((filter0 + filter) >> 4, a.n_tiles - 1);
+    const uint16_t* scales = a.scales + (long long)tile * a.n_groups * 16 + (filter & 15);
+    const int g0 = (b_first * 4) >> shift;
+    float acc[kMine];
+#pragma unroll
+    for (int q = 0; q < kMine; ++q) acc[q] = 0.f;
+    float s = n_sums > 0 ? bf16_float(__ldg(scales + g0 * 16)) : 0.f;
+    for (int n = 0; n < n_sums; ++n) {
+      const float next = bf16_float(__ldg(scales + min(g0 + n + 1, a.n_groups - 1) * 16));
+      const int buf = n % kSums;
+      if (!mbar_wait_warp(smem_u32(&mb->sum_full[buf]), uint32_t(n / kSums) & 1u, bars, err, 4)) break;
+      tc_fence_after();
+      const uint32_t at = tmem + (uint32_t(quad * 32) << 16) + buf * kCols + half * kMine;
+#pragma unroll
+      for (int c = 0; c < kMine; c += 32) {
+        uint32_t r[32];
+        tmem_ld32(at + c, r);
+#pragma unroll
+        for (int q = 0; q < 32; ++q) acc[c + q] = fmaf(s, __uint_as_float(r[q]), acc[c + q]);
+      }
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(smem_u32(&mb->sum_empty[buf]));
+      s = next;
+    }
+    const int i = filter0 + filter;
+    __nv_bfloat16* y = static_cast<__nv_bfloat16*>(a.y);
+    if (splits == 1) {
+      if (!bars->abort_flag && i < a.m) {
+        const float bias = a.bias ? __ldg(a.bias + i) : 0.f;
+#pragma unroll
+        for (int q = 0; q < kMine; ++q) {
+          const long long r = row0 + half * kMine + q;
+          const float v = acc[q] * 64.f + bias;
+          if (r < a.rows) y[r * a.y_pitch + i] = __float2bfloat16_rn(a.relu ? relu_of(v) : v);
+        }
+      }
+    } else {
+      // [column][filter], where the ring was: its copies have all been read
+      float* part = reinterpret_cast<float*>(ring);
+#pragma unroll
+      for (int q = 0; q < kMine; ++q) part[(half * kMine + q) * 128 + filter] = acc[q];
+      __syncwarp();
+      cluster_sync_all();
+      if (!bars->abort_flag && i < a.m) {
+        const float bias = a.bias ? __ldg(a.bias + i) : 0.f;
+        for (int c = split * kCols / splits + half; c < (split + 1) * kCols / splits; c += 2) {
+          float v = 0.f;
+          for (int q = 0; q < splits; ++q) v += ld_cluster_f32(mapa_shared(base + (c * 128 + filter) * 4, uint32_t(q)));
+          v = v * 64.f + bias;
+          if (row0 + c < a.rows) y[(row0 + c) * a.y_pitch + i] = __float2bfloat16_rn(a.relu ? relu_of(v) : v);
+        }
+      }
+    }
+  } else {
+    // ------------------------------------------------------------------ codes: a tile of 16 filters for each warp
+    const int w = warp - 2 - kResultWarps, g = lane >> 2, t = lane & 3;
+    const int tile = min((filter0 >> 4) + w, a.n_tiles - 1);
+    const uint4* codes = a.codes + ((long long)tile * a.k_blocks) * 32 + lane;
+    const uint8_t* zeros = kZeros ? a.zeros + (long long)tile * a.n_groups * 16 + g : nullptr;
+    // places of filter g: units t and 4 + t of its row of 128 bytes, swizzled; filter g + 8 lies 1024 bytes further.  Odd filters write
+    // the second unit first: eight lanes' 16 bytes then lie in eight columns.
+    const int odd = g & 1;
+    const uint32_t row = uint32_t(w * 16 + g) * 128, at0 = row + (((t + 4 * odd) ^ g) << 4), at1 = row + (((t + 4 * (odd ^ 1)) ^ g) << 4);
+    uint4 words[kAhead];
+    uint32_t z[kAhead][2][2] = {};                   // half, filter
+    auto fetch = [&](int slot, int b) {
+      if (b >= b_last) return;
+      words[slot] = __ldg(codes + (long long)b * 32);
+      if (kZeros) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int grp = min((b * 4 + 2 * h) >> shift, a.n_groups - 1);
+          z[slot][h][0] = __ldg(zeros + grp * 16); z[slot][h][1] = __ldg(zeros + grp * 16 + 8);
+        }
+      }
+    };
+#pragma unroll
+    for (int q = 0; q < kAhead; ++q) fetch(q, b_first + q);
+    int stage = 0;
+    uint32_t phase = 0;
+    bool ok = true;
+    for (int b0 = b_first; b0 < b_last && ok; b0 += kAhead) {
+#pragma unroll
+      for (int q = 0; q < kAhead; ++q) {
+        const int b = b0 + q;
+        if (b >= b_last) break;
+        const uint32_t w2[2][2] = {{words[q].x, words[q].y}, {words[q].z, words[q].w}};           // half, filter
+        uint32_t v[2][2][4];
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int f = 0; f < 2; ++f) spread_codes(w2[h][f], kZeros ? minus_zero(z[q][h][f]) : kMinusEighth, v[h][f]);
+        fetch(q, b + kAhead);
+        if (!mbar_wait_warp(smem_u32(&bars->empty[stage]), phase ^ 1u, bars, err, 5)) { ok = false; break; }
+        const uint32_t to = base + stage * S::kStage;
+#pragma unroll
+        for (int f = 0; f < 2; ++f)
+#pragma unroll
+          for (int n = 0; n < 2; ++n) {
+            const uint32_t at = to + (n ? at1 : at0) + f * 1024;
+            const bool second = (n ^ odd) != 0;
+            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(second ? v[1][f][0] : v[0][f][0]), "r"(second ? v[1][f][1] : v[0][f][1]),
+                         "r"(second ? v[1][f][2] : v[0][f][2]), "r"(second ? v[1][f][3] : v[0][f][3]) : "memory");
+          }
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&bars->full[stage]));
+        if (++stage == S::kRing) { stage = 0; phase ^= 1u; }
+      }
+    }
+  }
+  if (splits > 1) {
+    __syncwarp();
+    if (warp < 2 || warp >= 2 + kResultWarps) cluster_sync_all();
+    cluster_sync_all();                              // nobody leaves while its sums are still being read
+  }
+  if (bars->abort_flag) {
+    // give copies and products still in flight time to land before TMEM goes away
+    const long long t0 = clock64();
+    while (clock64() - t0 < 2000000ll) { }
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 1) {
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(uint32_t(kSums * kCols)) : "memory");
+  }
+}
+
+template <int kCols>
+rt3d_status launch_many(const LinearArgs& a, const DeviceInfo& dev, cudaStream_t st) {
+  typedef ManyShape<kCols> S;
+  CUtensorMap xmap;
+  const cuuint64_t dims[2] = {cuuint64_t(a.k), cuuint64_t(a.rows)}, strides[1] = {cuuint64_t(a.x_pitch) * 2};
+  const cuuint32_t box[2] = {64, kCols}, estr[2] = {1, 1};
+  if (encode_tiled(&xmap, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(a.x), dims, strides, box, estr, CU_TENSOR_MAP_SWIZZLE_128B) != CUDA_SUCCESS)
+    return RT3D_ERR_CUDA;
+  const auto kernel = a.zeros ? linear_w4_many_kernel<kCols, true> : linear_w4_many_kernel<kCols, false>;
+  static std::atomic<bool> attr_done[kMaxDevices][2];
+  const int d = current_device_index();
+  if (d < 0) return RT3D_ERR_CUDA;
+  std::atomic<bool>& done = attr_done[d][a.zeros != nullptr];
+  if (!done.load()) {
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(S::kBytes)) != cudaSuccess) return RT3D_ERR_CUDA;
+    done.store(true);
+  }
+  const int tiles = ceil_div(a.n_tiles, 8);
+  const long long row_tiles = ceil_div64(a.rows, kCols);
+  // the inputs are shared out while that fills SMs and leaves every CTA eight blocks
+  int splits = 1;
+  while (splits < 8 && tiles * row_tiles * splits * 2 <= dev.sm_count && a.k_blocks >= 16 * splits) splits *= 2;
+  LaunchSetup ls(dim3(unsigned(tiles * splits), unsigned(row_tiles)), dim3(kThreads), S::kBytes, st, unsigned(splits));
+  if (cudaLaunchKernelEx(&ls.cfg, kernel, xmap, a, splits, dev.err) != cudaSuccess) return RT3D_ERR_CUDA;
+  count_launches(1);
+  return RT3D_OK;
+}
+
+}  // namespace
+
+rt3d_status linear_w4_many_rows(const LinearArgs& a, const DeviceInfo& dev, cudaStream_t st) {
+  return a.rows <= 64 ? launch_many<64>(a, dev, st) : launch_many<128>(a, dev, st);
+}
+
+}  // namespace rt3d

@@ -262,7 +262,7 @@ w4_unpack_kernel(T* __restrict__ w, const GridArgs a) {
 // share the inputs further and add their sums up through one another's shared memory, always in the same order.
 constexpr int kLinearThreads = 256;
 constexpr int kMostRows = 1 << 19;                          // of a launch
-constexpr int kManyRows = 32;                               // more bf16 rows go to linear_w4_many_rows
+constexpr int kManyRows = 16;                               // more bf16 rows go to linear_w4_many_rows
 
 __device__ __forceinline__ void mma_bf16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
   asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"

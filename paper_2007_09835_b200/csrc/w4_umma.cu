@@ -31,7 +31,7 @@ namespace {
 constexpr int kResultWarps = 8, kCodeWarps = 8, kThreads = 32 * (2 + kResultWarps + kCodeWarps);
 constexpr int kSums = 4;                             // accumulators in tensor memory
 constexpr uint32_t kFilterBytes = 128 * 128;         // 128 filters x 64 bf16
-constexpr int kAhead = 4;                            // blocks of codes on their way to a warp
+constexpr int kAhead = 2;                            // stages of codes on their way to a warp
 
 struct ManyBars {
   Barriers b;                                        // full, empty: the ring
@@ -40,13 +40,16 @@ struct ManyBars {
 
 template <int kCols>
 struct ManyShape {
-  static constexpr uint32_t kStage = kFilterBytes + kCols * 128;
-  static constexpr int kRing = kCols == 64 ? 8 : 6;
+  // 128 inputs: two blocks of filters, two of rows.  (A stage of 64 left the thread that issues the products 1200 clocks a stage, twice
+  // what they take: 4096 x 8192, 256 rows, 41 us.)
+  static constexpr uint32_t kRowsAt = 2 * kFilterBytes, kStage = kRowsAt + 2 * kCols * 128;
+  static constexpr int kRing = kCols == 64 ? 4 : 3;
   static constexpr uint32_t kPart = 128 * kCols * 4, kBytes = kRing * kStage + 1024 + sizeof(ManyBars);
   static_assert(kPart <= kRing * kStage, "the sums go where the ring was");
 };
 
-template <int kCols, bool kZeros>
+// kShift: log2 of the 16s of inputs in a group.
+template <int kCols, bool kZeros, int kShift>
 __global__ void __launch_bounds__(kThreads, 1)
 linear_w4_many_kernel(const __grid_constant__ CUtensorMap xmap, const LinearArgs a, int splits, int32_t* __restrict__ err) {
   typedef ManyShape<kCols> S;
@@ -59,12 +62,11 @@ linear_w4_many_kernel(const __grid_constant__ CUtensorMap xmap, const LinearArgs
   const int split = splits > 1 ? int(cluster_ctarank()) : 0;
   const int filter0 = int(blockIdx.x) / splits * 128;
   const long long row0 = (long long)blockIdx.y * kCols;
-  // blocks of 64 inputs, in pairs so that no group is cut
+  // stages of 128 inputs, in which no group is cut
   const int pairs = (a.k_blocks + 1) / 2;
-  const int b_first = 2 * int((long long)pairs * split / splits), b_last = min(2 * int((long long)pairs * (split + 1) / splits), a.k_blocks);
-  // 16s of inputs in a group: 2, 4 or 8
-  const int shift = a.group_shift + 2 - (a.fine ? 1 : 0), per_group = 1 << shift;
-  const int n_sums = ((b_last - b_first) * 4 + per_group - 1) >> shift;
+  const int p_first = int((long long)pairs * split / splits), p_last = int((long long)pairs * (split + 1) / splits);
+  constexpr int kGroup16 = 1 << kShift, kGroups = 8 >> kShift;      // 16s in a group, groups in a stage
+  const int n_sums = (p_last - p_first) * kGroups;
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < S::kRing; ++s) { mbar_init(smem_u32(&bars->full[s]), 1 + kCodeWarps); mbar_init(smem_u32(&bars->empty[s]), 1); }
@@ -92,11 +94,12 @@ linear_w4_many_kernel(const __grid_constant__ CUtensorMap xmap, const LinearArgs
     if (lane == 0) {
       int stage = 0;
       uint32_t phase = 0;
-      for (int b = b_first; b < b_last; ++b) {
-        const uint32_t full = smem_u32(&bars->full[stage]);
+      for (int p = p_first; p < p_last; ++p) {
+        const uint32_t full = smem_u32(&bars->full[stage]), to = base + stage * S::kStage + S::kRowsAt;
         if (!mbar_wait(smem_u32(&bars->empty[stage]), phase ^ 1u, bars, err, 1)) break;
-        mbar_expect_tx(full, uint32_t(kCols) * 128);
-        tma_load_2d(base + stage * S::kStage + kFilterBytes, &xmap, full, b * 64, int(row0));
+        mbar_expect_tx(full, uint32_t(kCols) * 256);
+        tma_load_2d(to, &xmap, full, p * 128, int(row0));
+        tma_load_2d(to + kCols * 128, &xmap, full, p * 128 + 64, int(row0));
         if (++stage == S::kRing) { stage = 0; phase ^= 1u; }
       }
     }
@@ -104,26 +107,27 @@ linear_w4_many_kernel(const __grid_constant__ CUtensorMap xmap, const LinearArgs
     // ------------------------------------------------------------------ products
     const bool elected = elect_one();
     const uint32_t idesc = instr_desc_bf16(kCols);
-    int stage = 0, sum = 0;
-    uint32_t phase = 0;
+    int stage = 0;
+    uint32_t phase = 0, sum = 0;
     bool ok = true;
-    for (int b = b_first; b < b_last && ok; ++b) {
+    for (int p = p_first; p < p_last && ok; ++p) {
       if (!mbar_wait_warp(smem_u32(&bars->full[stage]), phase, bars, err, 2)) break;
       tc_fence_after();
       const uint32_t at = base + stage * S::kStage;
-      const uint64_t filters = smem_desc_sw128(at), rows = smem_desc_sw128(at + kFilterBytes);
+      const uint64_t filters = smem_desc_sw128(at), rows = smem_desc_sw128(at + S::kRowsAt);
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const int in = ((b - b_first) * 4 + k) & (per_group - 1);            // place in its group
-        const int buf = sum % kSums;
-        if (in == 0) {
-          if (!mbar_wait_warp(smem_u32(&mb->sum_empty[buf]), (uint32_t(sum / kSums) & 1u) ^ 1u, bars, err, 3)) { ok = false; break; }
-          tc_fence_after();
-        }
-        if (elected) umma_bf16(tmem + buf * kCols, filters + 2 * k, rows + 2 * k, idesc, in ? 1u : 0u);
-        if (in == per_group - 1 || (k == 3 && b + 1 == b_last)) {
-          if (elected) umma_commit(smem_u32(&mb->sum_full[buf]));
-          ++sum;
+      for (int g = 0; g < kGroups; ++g, ++sum) {
+        const uint32_t buf = sum % kSums;
+        if (!mbar_wait_warp(smem_u32(&mb->sum_empty[buf]), ((sum / kSums) & 1u) ^ 1u, bars, err, 3)) { ok = false; break; }
+        tc_fence_after();
+        if (elected) {
+#pragma unroll
+          for (int i = 0; i < kGroup16; ++i) {
+            const int k = g * kGroup16 + i;          // of the stage's eight 16s
+            umma_bf16(tmem + buf * kCols, filters + (k >> 2) * (kFilterBytes >> 4) + 2 * (k & 3), rows + (k >> 2) * (kCols * 128 >> 4) + 2 * (k & 3), idesc,
+                      i ? 1u : 0u);
+          }
+          umma_commit(smem_u32(&mb->sum_full[buf]));
         }
       }
       if (ok && elected) umma_commit(smem_u32(&bars->empty[stage]));
@@ -136,11 +140,11 @@ linear_w4_many_kernel(const __grid_constant__ CUtensorMap xmap, const LinearArgs
     const int quad = warp & 3, half = (warp - 2) >> 2, filter = quad * 32 + lane;
     const int tile = min((filter0 + filter) >> 4, a.n_tiles - 1);
     const uint16_t* scales = a.scales + (long long)tile * a.n_groups * 16 + (filter & 15);
-    const int g0 = (b_first * 4) >> shift;
+    const int g0 = p_first * kGroups;
     float acc[kMine];
 #pragma unroll
     for (int q = 0; q < kMine; ++q) acc[q] = 0.f;
-    float s = n_sums > 0 ? bf16_float(__ldg(scales + g0 * 16)) : 0.f;
+    float s = n_sums > 0 ? bf16_float(__ldg(scales + min(g0, a.n_groups - 1) * 16)) : 0.f;
     for (int n = 0; n < n_sums; ++n) {
       const float next = bf16_float(__ldg(scales + min(g0 + n + 1, a.n_groups - 1) * 16));
       const int buf = n % kSums;
@@ -198,47 +202,57 @@ linear_w4_many_kernel(const __grid_constant__ CUtensorMap xmap, const LinearArgs
     // the second unit first: eight lanes' 16 bytes then lie in eight columns.
     const int odd = g & 1;
     const uint32_t row = uint32_t(w * 16 + g) * 128, at0 = row + (((t + 4 * odd) ^ g) << 4), at1 = row + (((t + 4 * (odd ^ 1)) ^ g) << 4);
-    uint4 words[kAhead];
-    uint32_t z[kAhead][2][2] = {};                   // half, filter
-    auto fetch = [&](int slot, int b) {
-      if (b >= b_last) return;
-      words[slot] = __ldg(codes + (long long)b * 32);
-      if (kZeros) {
+    uint4 words[kAhead][2] = {};                     // of a block that is not there: anything, as x is zero there
+    uint32_t z[kAhead][2][2][2] = {};                // block, half, filter
+    auto fetch = [&](int slot, int p) {
+      if (p >= p_last) return;
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const int grp = min((b * 4 + 2 * h) >> shift, a.n_groups - 1);
-          z[slot][h][0] = __ldg(zeros + grp * 16); z[slot][h][1] = __ldg(zeros + grp * 16 + 8);
+      for (int d = 0; d < 2; ++d) {
+        const int b = 2 * p + d;
+        if (b < a.k_blocks) words[slot][d] = __ldg(codes + (long long)b * 32);
+        if (kZeros) {
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            if (kShift > 1 && h) { z[slot][d][1][0] = z[slot][d][0][0]; z[slot][d][1][1] = z[slot][d][0][1]; continue; }
+            const int grp = min((b * 4 + 2 * h) >> kShift, a.n_groups - 1);
+            z[slot][d][h][0] = __ldg(zeros + grp * 16); z[slot][d][h][1] = __ldg(zeros + grp * 16 + 8);
+          }
         }
       }
     };
 #pragma unroll
-    for (int q = 0; q < kAhead; ++q) fetch(q, b_first + q);
+    for (int q = 0; q < kAhead; ++q) fetch(q, p_first + q);
     int stage = 0;
     uint32_t phase = 0;
     bool ok = true;
-    for (int b0 = b_first; b0 < b_last && ok; b0 += kAhead) {
+    for (int p0 = p_first; p0 < p_last && ok; p0 += kAhead) {
 #pragma unroll
       for (int q = 0; q < kAhead; ++q) {
-        const int b = b0 + q;
-        if (b >= b_last) break;
-        const uint32_t w2[2][2] = {{words[q].x, words[q].y}, {words[q].z, words[q].w}};           // half, filter
-        uint32_t v[2][2][4];
+        if (p0 + q >= p_last) break;
+        uint32_t v[2][2][2][4];                      // block, unit as this lane writes them, filter: ready before the wait
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
+        for (int d = 0; d < 2; ++d)
 #pragma unroll
-          for (int f = 0; f < 2; ++f) spread_codes(w2[h][f], kZeros ? minus_zero(z[q][h][f]) : kMinusEighth, v[h][f]);
-        fetch(q, b + kAhead);
+          for (int n = 0; n < 2; ++n) {
+            const bool second = (n ^ odd) != 0;
+#pragma unroll
+            for (int f = 0; f < 2; ++f) {
+              const uint4& u = words[q][d];
+              const uint32_t w = second ? (f ? u.w : u.z) : (f ? u.y : u.x);
+              spread_codes(w, kZeros ? minus_zero(second ? z[q][d][1][f] : z[q][d][0][f]) : kMinusEighth, v[d][n][f]);
+            }
+          }
+        fetch(q, p0 + q + kAhead);
         if (!mbar_wait_warp(smem_u32(&bars->empty[stage]), phase ^ 1u, bars, err, 5)) { ok = false; break; }
         const uint32_t to = base + stage * S::kStage;
 #pragma unroll
-        for (int f = 0; f < 2; ++f)
+        for (int d = 0; d < 2; ++d)
 #pragma unroll
-          for (int n = 0; n < 2; ++n) {
-            const uint32_t at = to + (n ? at1 : at0) + f * 1024;
-            const bool second = (n ^ odd) != 0;
-            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(second ? v[1][f][0] : v[0][f][0]), "r"(second ? v[1][f][1] : v[0][f][1]),
-                         "r"(second ? v[1][f][2] : v[0][f][2]), "r"(second ? v[1][f][3] : v[0][f][3]) : "memory");
-          }
+          for (int f = 0; f < 2; ++f)
+#pragma unroll
+            for (int n = 0; n < 2; ++n)
+              asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + d * kFilterBytes + (n ? at1 : at0) + f * 1024), "r"(v[d][n][f][0]),
+                           "r"(v[d][n][f][1]), "r"(v[d][n][f][2]), "r"(v[d][n][f][3]) : "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncwarp();
         if (lane == 0) mbar_arrive(smem_u32(&bars->full[stage]));
@@ -272,11 +286,15 @@ rt3d_status launch_many(const LinearArgs& a, const DeviceInfo& dev, cudaStream_t
   const cuuint32_t box[2] = {64, kCols}, estr[2] = {1, 1};
   if (encode_tiled(&xmap, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(a.x), dims, strides, box, estr, CU_TENSOR_MAP_SWIZZLE_128B) != CUDA_SUCCESS)
     return RT3D_ERR_CUDA;
-  const auto kernel = a.zeros ? linear_w4_many_kernel<kCols, true> : linear_w4_many_kernel<kCols, false>;
-  static std::atomic<bool> attr_done[kMaxDevices][2];
+  typedef void (*Kernel)(CUtensorMap, LinearArgs, int, int32_t*);
+  static const Kernel kernels[2][3] = {{linear_w4_many_kernel<kCols, false, 1>, linear_w4_many_kernel<kCols, false, 2>, linear_w4_many_kernel<kCols, false, 3>},
+                                       {linear_w4_many_kernel<kCols, true, 1>, linear_w4_many_kernel<kCols, true, 2>, linear_w4_many_kernel<kCols, true, 3>}};
+  const int kind = a.fine ? 0 : a.group_shift + 1;
+  const Kernel kernel = kernels[a.zeros != nullptr][kind];
+  static std::atomic<bool> attr_done[kMaxDevices][2][3];
   const int d = current_device_index();
   if (d < 0) return RT3D_ERR_CUDA;
-  std::atomic<bool>& done = attr_done[d][a.zeros != nullptr];
+  std::atomic<bool>& done = attr_done[d][a.zeros != nullptr][kind];
   if (!done.load()) {
     if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(S::kBytes)) != cudaSuccess) return RT3D_ERR_CUDA;
     done.store(true);

@@ -28,7 +28,8 @@ CUresult encode_tiled(CUtensorMap* map, CUtensorMapDataType type, cuuint32_t ran
 
 namespace {
 
-constexpr int kResultWarps = 8, kCodeWarps = 8, kThreads = 32 * (2 + kResultWarps + kCodeWarps);
+constexpr int kCodeWarps = 8;
+constexpr int kMine = 32;                            // columns of a thread for the results
 constexpr int kSums = 4;                             // accumulators in tensor memory
 constexpr uint32_t kFilterBytes = 128 * 128;         // 128 filters x 64 bf16
 constexpr int kAhead = 2;                            // stages of codes on their way to a warp
@@ -44,15 +45,17 @@ struct ManyShape {
   // what they take: 4096 x 8192, 256 rows, 41 us.)
   static constexpr uint32_t kRowsAt = 2 * kFilterBytes, kStage = kRowsAt + 2 * kCols * 128;
   static constexpr int kRing = kCols == 64 ? 4 : 3;
+  static constexpr int kResultWarps = 4 * kCols / kMine, kThreads = 32 * (2 + kResultWarps + kCodeWarps);
   static constexpr uint32_t kPart = 128 * kCols * 4, kBytes = kRing * kStage + 1024 + sizeof(ManyBars);
   static_assert(kPart <= kRing * kStage, "the sums go where the ring was");
 };
 
 // kShift: log2 of the 16s of inputs in a group.
 template <int kCols, bool kZeros, int kShift>
-__global__ void __launch_bounds__(kThreads, 1)
+__global__ void __launch_bounds__(ManyShape<kCols>::kThreads, 1)
 linear_w4_many_kernel(const __grid_constant__ CUtensorMap xmap, const LinearArgs a, int splits, int32_t* __restrict__ err) {
   typedef ManyShape<kCols> S;
+  constexpr int kResultWarps = S::kResultWarps;
   extern __shared__ unsigned char smem_raw[];
   const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
   unsigned char* ring = smem_raw + (base - smem_u32(smem_raw));
@@ -136,7 +139,6 @@ linear_w4_many_kernel(const __grid_constant__ CUtensorMap xmap, const LinearArgs
     __syncwarp();
   } else if (warp < 2 + kResultWarps) {
     // ------------------------------------------------------------------ results
-    constexpr int kMine = kCols / 2;                 // columns of this thread
     const int quad = warp & 3, half = (warp - 2) >> 2, filter = quad * 32 + lane;
     const int tile = min((filter0 + filter) >> 4, a.n_tiles - 1);
     const uint16_t* scales = a.scales + (long long)tile * a.n_groups * 16 + (filter & 15);
@@ -151,16 +153,13 @@ linear_w4_many_kernel(const __grid_constant__ CUtensorMap xmap, const LinearArgs
       if (!mbar_wait_warp(smem_u32(&mb->sum_full[buf]), uint32_t(n / kSums) & 1u, bars, err, 4)) break;
       tc_fence_after();
       const uint32_t at = tmem + (uint32_t(quad * 32) << 16) + buf * kCols + half * kMine;
-#pragma unroll
-      for (int c = 0; c < kMine; c += 32) {
-        uint32_t r[32];
-        tmem_ld32(at + c, r);
-#pragma unroll
-        for (int q = 0; q < 32; ++q) acc[c + q] = fmaf(s, __uint_as_float(r[q]), acc[c + q]);
-      }
+      uint32_t r[32];
+      tmem_ld32(at, r);
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive(smem_u32(&mb->sum_empty[buf]));
+#pragma unroll
+      for (int q = 0; q < 32; ++q) acc[q] = fmaf(s, __uint_as_float(r[q]), acc[q]);
       s = next;
     }
     const int i = filter0 + filter;
@@ -184,7 +183,7 @@ linear_w4_many_kernel(const __grid_constant__ CUtensorMap xmap, const LinearArgs
       cluster_sync_all();
       if (!bars->abort_flag && i < a.m) {
         const float bias = a.bias ? __ldg(a.bias + i) : 0.f;
-        for (int c = split * kCols / splits + half; c < (split + 1) * kCols / splits; c += 2) {
+        for (int c = split * kCols / splits + half; c < (split + 1) * kCols / splits; c += kResultWarps / 4) {
           float v = 0.f;
           for (int q = 0; q < splits; ++q) v += ld_cluster_f32(mapa_shared(base + (c * 128 + filter) * 4, uint32_t(q)));
           v = v * 64.f + bias;
@@ -229,7 +228,8 @@ linear_w4_many_kernel(const __grid_constant__ CUtensorMap xmap, const LinearArgs
 #pragma unroll
       for (int q = 0; q < kAhead; ++q) {
         if (p0 + q >= p_last) break;
-        uint32_t v[2][2][2][4];                      // block, unit as this lane writes them, filter: ready before the wait
+        if (!mbar_wait_warp(smem_u32(&bars->empty[stage]), phase ^ 1u, bars, err, 5)) { ok = false; break; }
+        const uint32_t to = base + stage * S::kStage;
 #pragma unroll
         for (int d = 0; d < 2; ++d)
 #pragma unroll
@@ -239,20 +239,13 @@ linear_w4_many_kernel(const __grid_constant__ CUtensorMap xmap, const LinearArgs
             for (int f = 0; f < 2; ++f) {
               const uint4& u = words[q][d];
               const uint32_t w = second ? (f ? u.w : u.z) : (f ? u.y : u.x);
-              spread_codes(w, kZeros ? minus_zero(second ? z[q][d][1][f] : z[q][d][0][f]) : kMinusEighth, v[d][n][f]);
+              uint32_t v[4];
+              spread_codes(w, kZeros ? minus_zero(second ? z[q][d][1][f] : z[q][d][0][f]) : kMinusEighth, v);
+              asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + d * kFilterBytes + (n ? at1 : at0) + f * 1024), "r"(v[0]), "r"(v[1]),
+                           "r"(v[2]), "r"(v[3]) : "memory");
             }
           }
         fetch(q, p0 + q + kAhead);
-        if (!mbar_wait_warp(smem_u32(&bars->empty[stage]), phase ^ 1u, bars, err, 5)) { ok = false; break; }
-        const uint32_t to = base + stage * S::kStage;
-#pragma unroll
-        for (int d = 0; d < 2; ++d)
-#pragma unroll
-          for (int f = 0; f < 2; ++f)
-#pragma unroll
-            for (int n = 0; n < 2; ++n)
-              asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + d * kFilterBytes + (n ? at1 : at0) + f * 1024), "r"(v[d][n][f][0]),
-                           "r"(v[d][n][f][1]), "r"(v[d][n][f][2]), "r"(v[d][n][f][3]) : "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncwarp();
         if (lane == 0) mbar_arrive(smem_u32(&bars->full[stage]));
@@ -304,7 +297,7 @@ rt3d_status launch_many(const LinearArgs& a, const DeviceInfo& dev, cudaStream_t
   // the inputs are shared out while that fills SMs and leaves every CTA eight blocks
   int splits = 1;
   while (splits < 8 && tiles * row_tiles * splits * 2 <= dev.sm_count && a.k_blocks >= 16 * splits) splits *= 2;
-  LaunchSetup ls(dim3(unsigned(tiles * splits), unsigned(row_tiles)), dim3(kThreads), S::kBytes, st, unsigned(splits));
+  LaunchSetup ls(dim3(unsigned(tiles * splits), unsigned(row_tiles)), dim3(S::kThreads), S::kBytes, st, unsigned(splits));
   if (cudaLaunchKernelEx(&ls.cfg, kernel, xmap, a, splits, dev.err) != cudaSuccess) return RT3D_ERR_CUDA;
   count_launches(1);
   return RT3D_OK;

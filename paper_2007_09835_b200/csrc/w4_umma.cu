@@ -32,7 +32,7 @@ constexpr int kCodeWarps = 8;
 constexpr int kMine = 32;                            // columns of a thread for the results
 constexpr int kSums = 4;                             // accumulators in tensor memory
 constexpr uint32_t kFilterBytes = 128 * 128;         // 128 filters x 64 bf16
-constexpr int kAhead = 2;                            // stages of codes on their way to a warp
+constexpr int kAhead = 4;                            // stages of codes on their way to a warp
 
 struct ManyBars {
   Barriers b;                                        // full, empty: the ring
@@ -146,21 +146,31 @@ linear_w4_many_kernel(const __grid_constant__ CUtensorMap xmap, const LinearArgs
     float acc[kMine];
 #pragma unroll
     for (int q = 0; q < kMine; ++q) acc[q] = 0.f;
-    float s = n_sums > 0 ? bf16_float(__ldg(scales + min(g0, a.n_groups - 1) * 16)) : 0.f;
-    for (int n = 0; n < n_sums; ++n) {
-      const float next = bf16_float(__ldg(scales + min(g0 + n + 1, a.n_groups - 1) * 16));
-      const int buf = n % kSums;
-      if (!mbar_wait_warp(smem_u32(&mb->sum_full[buf]), uint32_t(n / kSums) & 1u, bars, err, 4)) break;
-      tc_fence_after();
-      const uint32_t at = tmem + (uint32_t(quad * 32) << 16) + buf * kCols + half * kMine;
-      uint32_t r[32];
-      tmem_ld32(at, r);
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(smem_u32(&mb->sum_empty[buf]));
+    // scales are asked for eight groups ahead: one ahead, every group waited 900 clocks for the next one's
+    constexpr int kScales = 8;
+    uint16_t scale[kScales];
+    auto scale_of = [&](int n) { return __ldg(scales + (long long)min(g0 + n, a.n_groups - 1) * 16); };
 #pragma unroll
-      for (int q = 0; q < 32; ++q) acc[q] = fmaf(s, __uint_as_float(r[q]), acc[q]);
-      s = next;
+    for (int q = 0; q < kScales; ++q) scale[q] = scale_of(q);
+    bool ok = true;
+    for (int n0 = 0; n0 < n_sums && ok; n0 += kScales) {
+#pragma unroll
+      for (int q = 0; q < kScales; ++q) {
+        const int n = n0 + q, buf = n % kSums;
+        if (n >= n_sums) break;
+        const float s = bf16_float(scale[q]);
+        scale[q] = scale_of(n + kScales);
+        if (!mbar_wait_warp(smem_u32(&mb->sum_full[buf]), uint32_t(n / kSums) & 1u, bars, err, 4)) { ok = false; break; }
+        tc_fence_after();
+        const uint32_t at = tmem + (uint32_t(quad * 32) << 16) + buf * kCols + half * kMine;
+        uint32_t r[32];
+        tmem_ld32(at, r);
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&mb->sum_empty[buf]));
+#pragma unroll
+        for (int e = 0; e < 32; ++e) acc[e] = fmaf(s, __uint_as_float(r[e]), acc[e]);
+      }
     }
     const int i = filter0 + filter;
     __nv_bfloat16* y = static_cast<__nv_bfloat16*>(a.y);
@@ -195,26 +205,30 @@ linear_w4_many_kernel(const __grid_constant__ CUtensorMap xmap, const LinearArgs
     // ------------------------------------------------------------------ codes: a tile of 16 filters for each warp
     const int w = warp - 2 - kResultWarps, g = lane >> 2, t = lane & 3;
     const int tile = min((filter0 >> 4) + w, a.n_tiles - 1);
-    const uint4* codes = a.codes + ((long long)tile * a.k_blocks) * 32 + lane;
-    const uint8_t* zeros = kZeros ? a.zeros + (long long)tile * a.n_groups * 16 + g : nullptr;
     // places of filter g: units t and 4 + t of its row of 128 bytes, swizzled; filter g + 8 lies 1024 bytes further.  Odd filters write
     // the second unit first: eight lanes' 16 bytes then lie in eight columns.
     const int odd = g & 1;
     const uint32_t row = uint32_t(w * 16 + g) * 128, at0 = row + (((t + 4 * odd) ^ g) << 4), at1 = row + (((t + 4 * (odd ^ 1)) ^ g) << 4);
-    uint4 words[kAhead][2] = {};                     // of a block that is not there: anything, as x is zero there
-    uint32_t z[kAhead][2][2][2] = {};                // block, half, filter
+    // Words and zero points come in the order in which they are written.
+    const uint2* codes = reinterpret_cast<const uint2*>(a.codes + ((long long)tile * a.k_blocks) * 32 + lane) + odd;
+    const int other = odd ? -1 : 1;                  // from the unit written first to the second
+    const uint8_t* zeros = kZeros ? a.zeros + (long long)tile * a.n_groups * 16 + g : nullptr;
+    constexpr int kZ = kShift > 1 ? 1 : 2;           // zero points of a block: one for both halves, or one each
+    uint2 words[kAhead][2][2] = {};                  // block, unit (filters g and g + 8); of a block that is not there: anything, as x is zero there
+    uint32_t z[kAhead][2][kZ] = {};                  // of both filters
     auto fetch = [&](int slot, int p) {
       if (p >= p_last) return;
 #pragma unroll
       for (int d = 0; d < 2; ++d) {
         const int b = 2 * p + d;
-        if (b < a.k_blocks) words[slot][d] = __ldg(codes + (long long)b * 32);
-        if (kZeros) {
+        if (b >= a.k_blocks) continue;
+        const uint2* src = codes + (long long)b * 64;
+        words[slot][d][0] = __ldg(src); words[slot][d][1] = __ldg(src + other);
+        if (kZeros && (d == 0 || kShift < 3)) {
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            if (kShift > 1 && h) { z[slot][d][1][0] = z[slot][d][0][0]; z[slot][d][1][1] = z[slot][d][0][1]; continue; }
-            const int grp = min((b * 4 + 2 * h) >> kShift, a.n_groups - 1);
-            z[slot][d][h][0] = __ldg(zeros + grp * 16); z[slot][d][h][1] = __ldg(zeros + grp * 16 + 8);
+          for (int h = 0; h < kZ; ++h) {
+            const int grp = kShift == 1 ? min(b * 2 + (h ^ odd), a.n_groups - 1) : kShift == 2 ? b : p;
+            z[slot][d][h] = __ldg(zeros + grp * 16) | uint32_t(__ldg(zeros + grp * 16 + 8)) << 16;
           }
         }
       }
@@ -230,17 +244,19 @@ linear_w4_many_kernel(const __grid_constant__ CUtensorMap xmap, const LinearArgs
         if (p0 + q >= p_last) break;
         if (!mbar_wait_warp(smem_u32(&bars->empty[stage]), phase ^ 1u, bars, err, 5)) { ok = false; break; }
         const uint32_t to = base + stage * S::kStage;
+        uint32_t minus[2] = {kMinusEighth, kMinusEighth};
 #pragma unroll
         for (int d = 0; d < 2; ++d)
 #pragma unroll
           for (int n = 0; n < 2; ++n) {
-            const bool second = (n ^ odd) != 0;
+            if (kZeros && n < kZ && (d == 0 || kShift < 3)) {
+              minus[0] = minus_zero(z[q][d][n < kZ ? n : 0] & 0xffffu);
+              minus[1] = minus_zero(z[q][d][n < kZ ? n : 0] >> 16);
+            }
 #pragma unroll
             for (int f = 0; f < 2; ++f) {
-              const uint4& u = words[q][d];
-              const uint32_t w = second ? (f ? u.w : u.z) : (f ? u.y : u.x);
               uint32_t v[4];
-              spread_codes(w, kZeros ? minus_zero(second ? z[q][d][1][f] : z[q][d][0][f]) : kMinusEighth, v);
+              spread_codes(f ? words[q][d][n].y : words[q][d][n].x, minus[f], v);
               asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + d * kFilterBytes + (n ? at1 : at0) + f * 1024), "r"(v[0]), "r"(v[1]),
                            "r"(v[2]), "r"(v[3]) : "memory");
             }

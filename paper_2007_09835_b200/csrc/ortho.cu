@@ -217,13 +217,15 @@ constexpr uint32_t kRowsBytes = kTile * 128;         // of 128 x 64 fp16
 constexpr int kProductThreads = 320;                 // producer, issuer, eight warps for the results
 constexpr int kMostProblems = 16;                    // of one launch
 
-// Tiles of 128 x kCols: a stage holds 64 of the sum of up to four operands (hi and lo of A and B).
+// Tiles of 128 x kCols: a stage holds 64 of the sum of up to four operands (hi and lo of A and B), as many as the launch's products have.
 template <int kCols>
 struct Stage {
-  static constexpr uint32_t kColsBytes = kCols * 128, kBAt = 2 * kRowsBytes, kBytes = 2 * kRowsBytes + 2 * kColsBytes;
-  static constexpr int kRing = 3;
+  static constexpr uint32_t kColsBytes = kCols * 128, kRingBytes = 3 * (2 * kRowsBytes + 2 * kColsBytes);
   // results on their way out (128 x 64): hi and lo
-  static constexpr uint32_t kOutAt = kRing * kBytes, kAllBytes = kCols == 64 ? kOutAt + 2 * kRowsBytes : kRing * kBytes;
+  static constexpr uint32_t kOutAt = kRingBytes, kAllBytes = kCols == 64 ? kOutAt + 2 * kRowsBytes : kRingBytes;
+  // columns of an accumulator: with both parts of B side by side, hi hi and hi lo are one product where kCols is 64 (120 clocks for 16 of
+  // the sum of all three parts, 168 one after another)
+  static constexpr int kAcc = 128;
 };
 
 enum { kOutParts = 0, kOutDirection = 1, kOutUpdate = 2 };
@@ -264,6 +266,8 @@ struct ProductArgs {
   Maps m[kMatrices];
   Steps<kProblems> steps;
   int n_steps, splits;
+  int ring;                                          // stages
+  uint32_t b_at, stage_bytes;
   int one_cluster;                                   // the grid is a cluster, which is what steps wait through
   unsigned* arrived;                                 // else: CTAs that have reached the ends of steps, all together
   // results outside
@@ -456,7 +460,7 @@ __device__ __forceinline__ void finish_staged(const Problem& p, const Maps* maps
     const int diagonal = p.symmetric ? t.i * kTile + row - t.j * kCols - half * 32 : -1;        // of this row's columns
     uint32_t r[32];
     __syncwarp();
-    tmem_ld32(taddr + half * 32, r);
+    tmem_ld_acc(taddr + half * 32, true, p.parts == 3 ? uint32_t(kCols) : 0u, r);
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
       const uint32_t at = line + (((half * 4 + u) ^ (row & 7)) << 4);
@@ -534,7 +538,7 @@ product_kernel(const __grid_constant__ ProductArgs<kProblems> a) {
   const int cta = int(blockIdx.x) / a.splits, n_ctas = int(gridDim.x) / a.splits;
 
   if (threadIdx.x == 0) {
-    for (int s = 0; s < S::kRing; ++s) { mbar_init(smem_u32(&bars->full[s]), 1); mbar_init(smem_u32(&bars->empty[s]), 1); }
+    for (int s = 0; s < a.ring; ++s) { mbar_init(smem_u32(&bars->full[s]), 1); mbar_init(smem_u32(&bars->empty[s]), 1); }
     for (int b = 0; b < 2; ++b) { mbar_init(smem_u32(&bars->tmem_full[b]), 1); mbar_init(smem_u32(&bars->tmem_empty[b]), 8); }
     mbar_init(smem_u32(&bars->full[kMaxStages - 1]), 1);         // of D
     bars->abort_flag = 0;
@@ -550,7 +554,7 @@ product_kernel(const __grid_constant__ ProductArgs<kProblems> a) {
     for (int q = int(threadIdx.x) - 64; q < (kProblems > 1 ? kMatrices * 4 : 0); q += kProductThreads - 64) tma_prefetch_map(&a.m[0].rows128[0] + q);
   if (warp == 1) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;"
-                 ::"r"(smem_u32(&bars->tmem_base)), "r"(uint32_t(2 * kCols)) : "memory");
+                 ::"r"(smem_u32(&bars->tmem_base)), "r"(uint32_t(2 * S::kAcc)) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
   tc_fence_before();
@@ -595,7 +599,7 @@ product_kernel(const __grid_constant__ ProductArgs<kProblems> a) {
         const uint32_t bytes = uint32_t(a_parts) * kRowsBytes + uint32_t(b_parts) * S::kColsBytes;
         const Maps& m = a.m[of_b ? p.b : p.a];
         const CUtensorMap *straight = of_b && kCols == 64 ? &m.rows64[q] : &m.rows128[q], *turned = &m.rows64[q];
-        const uint32_t to = base + (of_b ? S::kBAt + q * S::kColsBytes : q * kRowsBytes);
+        const uint32_t to = base + (of_b ? a.b_at + q * S::kColsBytes : q * kRowsBytes);
         const int at = of_b ? t.j * kCols : t.i * kTile, under = of_b ? p.b_under : p.a_under;
         const bool always = of_b && p.b_rows, mine = lane < 8 && q < (of_b ? b_parts : a_parts), wide = !of_b || kCols == kTile;
         const int c_last = p.chunks * (split + 1) / a.splits;
@@ -606,10 +610,10 @@ product_kernel(const __grid_constant__ ProductArgs<kProblems> a) {
           if (lane == 0) mbar_expect_tx(full, bytes);
           __syncwarp();
           if (mine && h <= (is_turned && wide ? 1 : 0)) {
-            if (is_turned) tma_load_2d(to + stage * S::kBytes + h * 8192, turned, full, at + 64 * h, c * 64);
-            else tma_load_2d(to + stage * S::kBytes, straight, full, c * 64, at);
+            if (is_turned) tma_load_2d(to + stage * a.stage_bytes + h * 8192, turned, full, at + 64 * h, c * 64);
+            else tma_load_2d(to + stage * a.stage_bytes, straight, full, c * 64, at);
           }
-          if (++stage == S::kRing) { stage = 0; phase ^= 1u; }
+          if (++stage == a.ring) { stage = 0; phase ^= 1u; }
         }
       }
       __syncwarp();
@@ -621,14 +625,14 @@ product_kernel(const __grid_constant__ ProductArgs<kProblems> a) {
         const TileAt t = item == cta ? t0 : tile_at<kCols>(steps, s, item);
         const Problem& p = steps.p[t.problem];
         const bool one = kCols == kTile && p.same && t.i == t.j;
-        const uint32_t buf = n & 1u, d = tmem + buf * kCols;
+        const uint32_t buf = n & 1u, d = tmem + buf * S::kAcc;
         if (!mbar_wait_warp(smem_u32(&bars->tmem_empty[buf]), ((n >> 1) & 1u) ^ 1u, bars, a.err, 2)) break;
         tc_fence_after();
         const int c_first = p.chunks * split / a.splits, c_last = p.chunks * (split + 1) / a.splits;
         for (int c = c_first; c < c_last; ++c) {
           if (!mbar_wait_warp(smem_u32(&bars->full[stage]), phase, bars, a.err, 3)) { ok = false; break; }
           tc_fence_after();
-          const uint32_t at = base + stage * S::kBytes, b_at = one ? at : at + S::kBAt, b_lo_at = one ? at + kRowsBytes : b_at + S::kColsBytes;
+          const uint32_t at = base + stage * a.stage_bytes, b_at = one ? at : at + a.b_at, b_lo_at = one ? at + kRowsBytes : b_at + S::kColsBytes;
           const bool a_turned = above(p.a_under, c, t.i * kTile), b_turned = p.b_rows || above(p.b_under, c, t.j * kCols);
           const uint32_t idesc = instr_desc_f16<kCols>(a_turned, b_turned);
           const uint64_t a_step = a_turned ? (16 * 128) >> 4 : 32 >> 4, b_step = b_turned ? (16 * 128) >> 4 : 32 >> 4;      // 16 of the sum
@@ -637,17 +641,25 @@ product_kernel(const __grid_constant__ ProductArgs<kProblems> a) {
           const uint64_t b_hi = b_turned ? smem_desc_rows(b_at) : smem_desc_sw128(b_at);
           const uint64_t b_lo = b_turned ? smem_desc_rows(b_lo_at) : smem_desc_sw128(b_lo_at);
           if (elected) {
+            const bool both = kCols == 64 && p.parts == 3;
+            const uint32_t more = c > c_first ? 1u : 0u;
+            if (both) {                              // hi hi and hi lo side by side
+              const uint32_t wide = instr_desc_f16<128>(a_turned, b_turned);
+#pragma unroll
+              for (int k = 0; k < 4; ++k) umma_bf16(d, a_hi + a_step * k, b_hi + b_step * k, wide, k ? 1u : more);
+            } else {
+#pragma unroll
+              for (int k = 0; k < 4; ++k) umma_bf16(d, a_hi + a_step * k, b_hi + b_step * k, idesc, k ? 1u : more);
+              if (p.parts == 3)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) umma_bf16(d, a_hi + a_step * k, b_lo + b_step * k, idesc, 1u);
+            }
             if (p.parts >= 2)
 #pragma unroll
-              for (int k = 0; k < 4; ++k) umma_bf16(d, a_lo + a_step * k, b_hi + b_step * k, idesc, c > c_first || k ? 1u : 0u);
-            if (p.parts == 3)
-#pragma unroll
-              for (int k = 0; k < 4; ++k) umma_bf16(d, a_hi + a_step * k, b_lo + b_step * k, idesc, 1u);
-#pragma unroll
-            for (int k = 0; k < 4; ++k) umma_bf16(d, a_hi + a_step * k, b_hi + b_step * k, idesc, c > c_first || k || p.parts >= 2 ? 1u : 0u);
+              for (int k = 0; k < 4; ++k) umma_bf16(d, a_lo + a_step * k, b_hi + b_step * k, idesc, 1u);
             umma_commit(smem_u32(&bars->empty[stage]));
           }
-          if (++stage == S::kRing) { stage = 0; phase ^= 1u; }
+          if (++stage == a.ring) { stage = 0; phase ^= 1u; }
         }
         if (!ok) break;
         if (elected) umma_commit(smem_u32(&bars->tmem_full[buf]));
@@ -660,7 +672,7 @@ product_kernel(const __grid_constant__ ProductArgs<kProblems> a) {
         const TileAt t = item == cta ? t0 : tile_at<kCols>(steps, s, item);
         const Problem& p = steps.p[t.problem];
         const float alpha = p.factor ? p.alpha * __ldcg(p.factor) : p.alpha;
-        const uint32_t buf = n & 1u, at = tmem + (uint32_t(quad * 32) << 16) + buf * kCols;
+        const uint32_t buf = n & 1u, at = tmem + (uint32_t(quad * 32) << 16) + buf * S::kAcc;
         Addend d;
         const long long d_at = (t.i * kTile + row) * p.pitch + t.j * kCols;
         if (kCols == 64 && p.out == kOutParts) {
@@ -685,6 +697,11 @@ product_kernel(const __grid_constant__ ProductArgs<kProblems> a) {
             float v[16];
 #pragma unroll
             for (int e = 0; e < 16; ++e) v[e] = __uint_as_float(r[e]);
+            if (kCols == 64 && p.parts == 3) {
+              tmem_ld16(at + kCols + c0, r);
+#pragma unroll
+              for (int e = 0; e < 16; ++e) v[e] += __uint_as_float(r[e]);
+            }
             finish16<kCols>(a, p, t, row, c0, v, alpha, d);
           }
         }
@@ -735,7 +752,7 @@ product_kernel(const __grid_constant__ ProductArgs<kProblems> a) {
   __syncthreads();
   if (warp == 1) {
     tc_fence_after();
-    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(uint32_t(2 * kCols)) : "memory");
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(uint32_t(2 * S::kAcc)) : "memory");
   }
 }
 
@@ -910,6 +927,15 @@ struct Runner {
       if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(kProductSmem<kCols>)) != cudaSuccess) return RT3D_ERR_CUDA;
       attr_done[d].store(true);
     }
+    int a_parts = 1, b_parts = 1;
+    for (int i = 0; i < a.steps.first[a.n_steps]; ++i) {
+      if (a.steps.p[i].parts >= 2) a_parts = 2;
+      if (a.steps.p[i].parts == 3) b_parts = 2;
+    }
+    a.b_at = a_parts * kRowsBytes;
+    a.stage_bytes = a.b_at + b_parts * Stage<kCols>::kColsBytes;
+    a.ring = int(Stage<kCols>::kRingBytes / a.stage_bytes);
+    if (a.ring > kMaxStages - 1) a.ring = kMaxStages - 1;                      // the last barrier is D's
     a.err = dev.err;
     std::memcpy(a.m, maps, sizeof(maps));
     LaunchSetup ls(dim3(unsigned(grid)), dim3(kProductThreads), kProductSmem<kCols>, st, cluster);

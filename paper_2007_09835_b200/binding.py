@@ -623,13 +623,18 @@ class W4Weights:
         device = self.codes.device
         tiles = (-(-self.m // 16), -(-self.k // self.group), 16)
         self.scales = torch.empty(tiles, dtype=torch.bfloat16, device=device) if scales is None else scales
-        self.zeros = torch.empty(tiles, dtype=torch.uint8, device=device) if zeros is True else zeros or None if isinstance(zeros, bool) else zeros
+        self.zeros = torch.empty(tiles, dtype=torch.uint8, device=device) if zeros is True else None if zeros is False else zeros
         for name, t, dtype, count in (("codes", self.codes, torch.uint8, n_bytes), ("scales", self.scales, torch.bfloat16, n_scales),
                                       ("zeros", self.zeros, torch.uint8, n_scales)):
             if t is not None and (t.dtype != dtype or t.numel() != count or not t.is_contiguous() or t.device != device):
                 raise ValueError(f"{name}: {count} contiguous values of {dtype} on {device} wanted")
         self.desc = W4(self.m, self.k, self.group, self.codes.data_ptr(), self.scales.data_ptr(),
                        None if self.zeros is None else self.zeros.data_ptr())
+
+    def __setattr__(self, name, value):
+        if "desc" in self.__dict__:                 # which holds their addresses
+            raise AttributeError("the arrays of 4-bit weights are written in place, not replaced")
+        object.__setattr__(self, name, value)
 
 
 def rt3d_w4_quantize(w, q: W4Weights, stream=None):

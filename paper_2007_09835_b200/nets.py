@@ -20,7 +20,8 @@ _pycall, _ADDRESS = B.pycall(), B.ADDRESS
 # The binding's compute functions as they are: calls go round them only while they are what the binding's module holds (a
 # tracer or a test that wraps them sees every call).
 _FUNCTIONS = {fn: getattr(B, fn) for fn in ("rt3d_conv3d_sparse", "rt3d_conv3d_dense", "rt3d_conv3d_sparse_fused",
-                                            "rt3d_conv2plus1d_fused", "rt3d_maxpool3d", "rt3d_add_relu", "rt3d_copy_f32")}
+                                            "rt3d_conv2plus1d_fused", "rt3d_maxpool3d", "rt3d_add_relu", "rt3d_copy_f32",
+                                            "rt3d_linear_w4")}
 
 
 def _unwrapped(*names) -> bool:
@@ -126,6 +127,52 @@ class ConvLayer:
         return B.rt3d_conv3d_cost(B.tensor_desc(x, self.spec.cin), self.packed, self.spec.stride, self.spec.pad)
 
 
+class LinearW4Layer:
+    """A fully connected (1x1x1) layer with 4-bit weights (rt3d_linear_w4), to stand among the `fc_layers` of a C3DNet in the place
+    of a dense ConvLayer.  `w`: the weights [M][N][1][1][1] or [M][N] (numpy or a device tensor, float32 or bfloat16), quantised
+    here on the device, or ready W4Weights.  Weights are quantised again in place by `quantize`."""
+
+    def __setattr__(self, name, value):
+        global _layer_changes
+        object.__setattr__(self, name, value)
+        _layer_changes = next(_changes)             # passes that were noted with the layer as it was are dropped
+
+    def __init__(self, spec, w, bias, group=128, zeros=False, dtype=torch.bfloat16, device="cuda"):
+        if tuple(spec.k) != (1, 1, 1) or tuple(spec.stride) != (1, 1, 1) or any(spec.pad):
+            raise ValueError("a fully connected layer is a 1x1x1 convolution without stride and padding")
+        self.spec, self.dtype, self.device = spec, dtype, device
+        if isinstance(w, B.W4Weights):
+            if (w.m, w.k) != (spec.cout, spec.cin):
+                raise ValueError("the weights' extents are not the layer's")
+            self.weights = w
+        else:
+            self.weights = B.W4Weights(spec.cout, spec.cin, group, zeros=zeros, device=device)
+            self.quantize(w)
+        if bias is not None and not isinstance(bias, torch.Tensor):
+            bias = torch.from_numpy(np.ascontiguousarray(bias, np.float32))
+        self.bias = None if bias is None else bias.to(device=device, dtype=torch.float32).contiguous()
+
+    def quantize(self, w, stream=None):
+        """New weights into the layer's codes and scales."""
+        if not isinstance(w, torch.Tensor):
+            w = torch.from_numpy(np.ascontiguousarray(w, np.float32))
+        B.rt3d_w4_quantize(w.to(self.device), self.weights, stream)
+
+    def out_shape(self, x: torch.Tensor):
+        return tuple(x.shape[:4]) + (pitch_for(self.spec.cout, self.dtype),)
+
+    def alloc_out(self, x: torch.Tensor) -> torch.Tensor:
+        return torch.zeros(self.out_shape(x), dtype=self.dtype, device=x.device)
+
+    def __call__(self, x: torch.Tensor, y: torch.Tensor | None = None, algo=B.ALGO_AUTO, relu=None, stream=None,
+                 x_pad_zero=False):
+        """The arguments of a ConvLayer; there is one kernel family, and x's padding never matters."""
+        if y is None:
+            y = self.alloc_out(x)
+        B.rt3d_linear_w4(x, self.weights, self.bias, y, self.spec.relu if relu is None else relu, stream)
+        return y
+
+
 def maxpool(x: torch.Tensor, c: int, pool, y: torch.Tensor | None = None, stream=None) -> torch.Tensor:
     n, t, h, w, cs = x.shape
     ext = [(d + 2 * p - k) // s + 1 for d, p, k, s in zip((t, h, w), pool.pad, pool.k, pool.stride)]
@@ -224,7 +271,7 @@ class C3DNet(_NotedForward):
     def __init__(self, plan, layers, fuse_pool: bool = False, input_pad_zero: bool = True, fc_layers=None):
         self.plan = plan
         self.layers = layers
-        self.fc_layers = fc_layers      # optional list of dense 1x1x1 ConvLayer (fc6, fc7, fc8) run on the flattened pool5 block
+        self.fc_layers = fc_layers      # optional list of dense 1x1x1 ConvLayer or LinearW4Layer (fc6, fc7, fc8) run on the flattened pool5 block
         self.fuse_pool = fuse_pool      # conv + ReLU + un-padded 2-wide max-pool in one launch where the library can
         self.input_pad_zero = input_pad_zero    # the clip tensor comes from to_device(): channels 3..7 are zeros
         self.ws = Workspace()

@@ -347,8 +347,9 @@ rt3d_status rt3d_kgs_expand_mask(const uint8_t* group_mask, int M, int N, int Kt
  * zero point (8 where `zeros` is NULL).  All arrays DEVICE, caller-owned, 16-byte aligned.  Layout: tiles of 16 filters x 64
  * inputs, 512 bytes each, [ceil(m/16)][ceil(k/64)] of them; in a tile the 16 bytes at 16 (4 g + t), g < 8, t < 4, are four
  * little-endian words: filter g, filter g + 8 (inputs 8 t .. 8 t + 7 of the tile), and the same filters with inputs 32 further on.
- * Input e < 8 of a word is at bits 4 ((e >> 1) + 4 (e & 1)) .. + 3.  Codes of filters or inputs that do not exist are written as the
- * zero point (8 for filters) and never reach a result.  Scales and zero points: [ceil(m/16)][ceil(k/group)][16].
+ * Input e < 8 of a word is at bits 4 ((e >> 1) + 4 (e & 1)) .. + 3.  Codes of inputs that do not exist are written as the filter's last zero
+ * point, those of filters that do not exist as 8, and never reach a result.  Scales and zero points: [ceil(m/16)][ceil(k/group)][16],
+ * both 0 for filters that do not exist.
  */
 typedef struct {
   int32_t m, k;          /* filters (outputs), inputs                                            */
@@ -394,13 +395,15 @@ rt3d_status rt3d_linear_w4(const rt3d_tensor* x, const rt3d_w4* q, const float* 
  *       w <- mask ((1 - lr weight_decay) w - lr scale O(u)).
  *   mask uint8 (nonzero = kept, the form of rt3d_kgs_expand_mask) or NULL; where it is zero, w and momentum become zero whatever
  *   w, momentum and g hold there.
- * Products take 16-bit parts of the values on the tensor cores with fp32 sums: two parts (22 bits) of every value for
- * rt3d_ortho_update and for the small matrices of both; results are within 1e-4 |O| of the exact ones in the Frobenius norm where
- * not rounded to bf16.  A gradient with an infinity or a NaN gives NaN (where the mask keeps anything), one of zeros gives zeros.
+ * Products take fp16 parts of the values on the tensor cores, with fp32 sums.  The direction of rt3d_ortho_update has two parts
+ * (22 bits) of every value throughout and is within 1e-4 |O| of the exact one (Frobenius norm, sides up to 2^18).  rt3d_orthogonalize
+ * rounds what its last steps start from to one part, 2^-12 of each value, and its result to bf16: within 3e-3 |O| and that rounding.
+ * A gradient with an infinity or a NaN gives NaN (where the mask keeps anything), one of zeros gives zeros.
  *   steps 1..16; coefs HOST [steps][3] (a, b, c of each step) or NULL for 3.4445, -4.7750, 2.0315; they must keep every singular
  *   value of [0, 1] below 1.9 in every step and |a + b s + c s s| at most 50, else UNSUPPORTED.  eps > 0.  p NULL: 5 steps, eps 1e-7.
  * rt3d_ortho_workspace: bytes of the workspace both calls need (16-byte aligned, caller-owned, contents of no meaning between
  *   calls; two calls that may overlap on the GPU, or two captured graphs that may, need one each); -1 for m or k < 1 or too large.
+ *   No array of a call may overlap another one of it, except that momentum and w are updated in place.
  * Both enqueue on `stream`, allocate nothing and do not synchronise.  The same inputs give the same bits.
  * Errors: INVALID_ARG, WORKSPACE (too few bytes), UNSUPPORTED (compute capability other than 10.x, coefficients), CUDA.
  */

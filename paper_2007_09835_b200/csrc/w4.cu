@@ -20,8 +20,6 @@ __device__ __forceinline__ uint32_t cluster_size() {
   return r;
 }
 
-__device__ __forceinline__ void store_value(float* p, float v) { *p = v; }
-__device__ __forceinline__ void store_value(__nv_bfloat16* p, float v) { *p = __float2bfloat16_rn(v); }
 
 __device__ __forceinline__ int shift_of(int e) { return 4 * ((e >> 1) + 4 * (e & 1)); }
 
@@ -180,7 +178,7 @@ w4_quantize_kernel(const T* __restrict__ w, const GridArgs a) {
       if (t == 0 && group < a.n_groups) {
         const long long at = (tile * a.n_groups + group) * 16 + g + 8 * f;
         a.scales[at] = q.bits;
-        if (a.zeros) a.zeros[at] = uint8_t(q.zero);
+        if (a.zeros) a.zeros[at] = i < a.m ? uint8_t(q.zero) : 0;
       }
       // places that do not exist hold zeros; behind the last group they have its zero point
       const float inv = __fdiv_rn(1.f, q.scale);
@@ -262,7 +260,7 @@ w4_unpack_kernel(T* __restrict__ w, const GridArgs a) {
 // share the inputs further and add their sums up through one another's shared memory, always in the same order.
 constexpr int kLinearThreads = 256;
 constexpr int kMostRows = 1 << 19;                          // of a launch
-constexpr int kManyRows = 16;                               // more bf16 rows go to linear_w4_many_rows
+constexpr int kManyRows = 16;                               // more go to linear_w4_many_rows
 
 __device__ __forceinline__ void mma_bf16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
   asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
@@ -293,27 +291,12 @@ struct Operand<__nv_bfloat16> {
 template <>
 struct Operand<float> {
   static constexpr int kParts = 3, kUnits = 2;
-  // The upper 8 bits of the mantissa, the next 8 and the last 8: each part is the rest's leading bits, so the three add up to the
-  // value and none is larger than it.  An infinity has no rest; a NaN's is a NaN.
   static __device__ __forceinline__ void read(const unsigned char* at, uint32_t (&b)[kParts][4]) {
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
-      const uint4 v = *reinterpret_cast<const uint4*>(at + u * 512);
-      const uint32_t f[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-      for (int p = 0; p < 2; ++p) {
-        uint32_t bits[3][2];
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          const float x = __uint_as_float(f[2 * p + e]);
-          const uint32_t h = f[2 * p + e] & 0xffff0000u;
-          const float r = fabsf(x) == __int_as_float(0x7f800000) ? 0.f : x - __uint_as_float(h);
-          const uint32_t m = __float_as_uint(r) & 0xffff0000u;
-          bits[0][e] = h; bits[1][e] = m; bits[2][e] = __float_as_uint(r - __uint_as_float(m));
-        }
-#pragma unroll
-        for (int q = 0; q < 3; ++q) b[q][2 * u + p] = __byte_perm(bits[q][0], bits[q][1], 0x7632);
-      }
+      const float4 v = *reinterpret_cast<const float4*>(at + u * 512);
+      split_pair(v.x, v.y, b[0][2 * u], b[1][2 * u], b[2][2 * u]);
+      split_pair(v.z, v.w, b[0][2 * u + 1], b[1][2 * u + 1], b[2][2 * u + 1]);
     }
   }
 };
@@ -684,20 +667,18 @@ rt3d_status linear(const rt3d_tensor* x, const rt3d_w4* q, const float* bias, in
     }
     return RT3D_OK;
   }
-  if (sizeof(T) == 2 && rows > kManyRows) return linear_w4_many_rows(a, dev, st);
-  // fp32 rows take three times the registers: 16 at a time at most, in two tiles
-  constexpr bool kWide = sizeof(T) == 2;
-  const int rows8 = rows <= 8 ? 1 : rows <= 16 || !kWide ? 2 : 4;
-  const int most = rows8 == 4 || (rows8 == 2 && !kWide) ? 2 : 4;
+  if (rows > kManyRows) return linear_w4_many_rows(a, x->dtype, dev, st);
+  const int rows8 = rows <= 8 ? 1 : 2;
+  // tiles of a CTA at most: sixteen fp32 rows take three times the registers of bf16 ones
+  const int most = rows8 == 2 && sizeof(T) == 4 ? 2 : 4;
   // One CTA an SM for up to two tiles each (4096 x 8192, one row: 7.3 us as 256 CTAs, 7.3 as 148; 16 rows: 12.0 and 10.7), two for
   // more (16384 x 16384, 4 rows: 37.4 us as 342 CTAs of up to 3 tiles, 30.3 as 296 of up to 4).  With fewer tiles than that, the CTAs
   // of a cluster share the inputs while every warp keeps eight blocks (16384 inputs of 1000 filters, one row: 7.9 us alone, 5.9
   // shared by four; 4096 inputs of 487: 4.0 alone, 4.2 by two).
   const int ctas = a.n_tiles <= sms ? a.n_tiles : a.n_tiles <= 2 * sms ? sms : 2 * sms * ceil_div(a.n_tiles, most * 2 * sms);
   int ranks = 1;
-  while (ranks < 8 && ctas < sms && ctas * ranks <= sms && rows <= rows8 * 8 && a.k_blocks >= 128 * ranks) ranks *= 2;
+  while (ranks < 8 && ctas < sms && ctas * ranks <= sms && a.k_blocks >= 128 * ranks) ranks *= 2;
   const int tiles = ceil_div(a.n_tiles, ctas);
-  if (tiles > most) return RT3D_ERR_UNSUPPORTED;
   const bool fine = q->group == 32;
   if (rows8 == 1) {
     if (tiles == 1) return launch_linear<T, 1, 1>(a, fine, ctas, ranks, st);
@@ -705,12 +686,12 @@ rt3d_status linear(const rt3d_tensor* x, const rt3d_w4* q, const float* bias, in
     if (tiles == 3) return launch_linear<T, 3, 1>(a, fine, ctas, ranks, st);
     return launch_linear<T, 4, 1>(a, fine, ctas, ranks, st);
   }
-  if constexpr (kWide) {
-    if (rows8 == 4) return tiles == 2 ? launch_linear<T, 2, 4>(a, fine, ctas, ranks, st) : launch_linear<T, 1, 4>(a, fine, ctas, ranks, st);
+  if (tiles == 1) return launch_linear<T, 1, 2>(a, fine, ctas, ranks, st);
+  if constexpr (sizeof(T) == 2) {
     if (tiles == 3) return launch_linear<T, 3, 2>(a, fine, ctas, ranks, st);
     if (tiles == 4) return launch_linear<T, 4, 2>(a, fine, ctas, ranks, st);
   }
-  return tiles == 2 ? launch_linear<T, 2, 2>(a, fine, ctas, ranks, st) : launch_linear<T, 1, 2>(a, fine, ctas, ranks, st);
+  return launch_linear<T, 2, 2>(a, fine, ctas, ranks, st);
 }
 
 }  // namespace

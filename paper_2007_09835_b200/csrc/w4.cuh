@@ -22,8 +22,8 @@ struct LinearArgs {
   int rows;
 };
 
-// Many bf16 rows (w4_umma.cu), at most 2^22.
-rt3d_status linear_w4_many_rows(const LinearArgs& a, const DeviceInfo& dev, cudaStream_t st);
+// Many rows (w4_umma.cu), at most 2^22.
+rt3d_status linear_w4_many_rows(const LinearArgs& a, int dtype, const DeviceInfo& dev, cudaStream_t st);
 
 namespace {
 
@@ -53,6 +53,25 @@ __device__ __forceinline__ void spread_codes(uint32_t w, uint32_t minus, uint32_
   v[2] = fma_bf16x2(u & 0x000F000Fu, kTwo127, minus);
   v[3] = fma_bf16x2(u & 0x00F000F0u, kTwo123, minus);
 }
+// Three bf16 parts of two values, packed: the upper 8 bits of the mantissa, the next 8 and the last 8.  Each part is the rest's leading bits,
+// so the three add up to the value and none is larger than it.  An infinity has no rest; a NaN's is a NaN.
+__device__ __forceinline__ void split_pair(float x, float y, uint32_t& hi, uint32_t& mid, uint32_t& lo) {
+  const float v[2] = {x, y};
+  uint32_t bits[3][2];
+#pragma unroll
+  for (int e = 0; e < 2; ++e) {
+    const uint32_t h = __float_as_uint(v[e]) & 0xffff0000u;
+    const float r = fabsf(v[e]) == __int_as_float(0x7f800000) ? 0.f : v[e] - __uint_as_float(h);
+    const uint32_t m = __float_as_uint(r) & 0xffff0000u;
+    bits[0][e] = h; bits[1][e] = m; bits[2][e] = __float_as_uint(r - __uint_as_float(m));
+  }
+  hi = __byte_perm(bits[0][0], bits[0][1], 0x7632);
+  mid = __byte_perm(bits[1][0], bits[1][1], 0x7632);
+  lo = __byte_perm(bits[2][0], bits[2][1], 0x7632);
+}
+
+__device__ __forceinline__ void store_value(float* p, float v) { *p = v; }
+__device__ __forceinline__ void store_value(__nv_bfloat16* p, float v) { *p = __float2bfloat16_rn(v); }
 
 }  // namespace
 }  // namespace rt3d

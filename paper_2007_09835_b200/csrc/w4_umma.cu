@@ -1,4 +1,4 @@
-// Products of many bf16 rows with 4-bit weights, on tcgen05.
+// Products of many rows with 4-bit weights, on tcgen05.
 //
 // As in w4.cu a group's sum of (c - z) x is exact but for the fp32 additions, and its scale multiplies it in fp32: so every group has
 // an accumulator of its own in tensor memory, which the warps for the results drain into registers, times the scale of their filter,
@@ -14,6 +14,7 @@
 #include <atomic>
 #include <cstdint>
 #include <cstring>
+#include <type_traits>
 
 #include "pdl.cuh"
 #include "rt3d.h"
@@ -39,22 +40,25 @@ struct ManyBars {
   unsigned long long sum_full[kSums], sum_empty[kSums];
 };
 
-template <int kCols>
+// Of bf16 rows one operand, by TMA; fp32 rows are split into three bf16 parts that add up to the value by warps of their own (w4.cuh).
+template <int kCols, bool kFloat>
 struct ManyShape {
+  static constexpr int kParts = kFloat ? 3 : 1, kRowWarps = kFloat ? 8 : 0;
   // 128 inputs: two blocks of filters, two of rows.  (A stage of 64 left the thread that issues the products 1200 clocks a stage, twice
   // what they take: 4096 x 8192, 256 rows, 41 us.)
-  static constexpr uint32_t kRowsAt = 2 * kFilterBytes, kStage = kRowsAt + 2 * kCols * 128;
-  static constexpr int kRing = kCols == 64 ? 4 : 3;
-  static constexpr int kResultWarps = 4 * kCols / kMine, kThreads = 32 * (2 + kResultWarps + kCodeWarps);
-  static constexpr uint32_t kPart = 128 * kCols * 4, kBytes = kRing * kStage + 1024 + sizeof(ManyBars);
-  static_assert(kPart <= kRing * kStage, "the sums go where the ring was");
+  static constexpr uint32_t kRowsAt = 2 * kFilterBytes, kPartBytes = 2 * kCols * 128, kStage = kRowsAt + kParts * kPartBytes;
+  static constexpr int kRing = kFloat ? 2 : kCols == 64 ? 4 : 3;
+  static constexpr int kResultWarps = 4 * kCols / kMine, kThreads = 32 * (2 + kResultWarps + kCodeWarps + kRowWarps);
+  static constexpr uint32_t kSumBytes = 128 * kCols * 4, kBytes = kRing * kStage + 1024 + sizeof(ManyBars);
+  static_assert(kSumBytes <= kRing * kStage, "the sums go where the ring was");
 };
 
 // kShift: log2 of the 16s of inputs in a group.
-template <int kCols, bool kZeros, int kShift>
-__global__ void __launch_bounds__(ManyShape<kCols>::kThreads, 1)
+template <int kCols, bool kFloat, bool kZeros, int kShift>
+__global__ void __launch_bounds__((ManyShape<kCols, kFloat>::kThreads), 1)
 linear_w4_many_kernel(const __grid_constant__ CUtensorMap xmap, const LinearArgs a, int splits, int32_t* __restrict__ err) {
-  typedef ManyShape<kCols> S;
+  typedef ManyShape<kCols, kFloat> S;
+  typedef typename std::conditional<kFloat, float, __nv_bfloat16>::type T;
   constexpr int kResultWarps = S::kResultWarps;
   extern __shared__ unsigned char smem_raw[];
   const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
@@ -72,13 +76,13 @@ linear_w4_many_kernel(const __grid_constant__ CUtensorMap xmap, const LinearArgs
   const int n_sums = (p_last - p_first) * kGroups;
 
   if (threadIdx.x == 0) {
-    for (int s = 0; s < S::kRing; ++s) { mbar_init(smem_u32(&bars->full[s]), 1 + kCodeWarps); mbar_init(smem_u32(&bars->empty[s]), 1); }
+    for (int s = 0; s < S::kRing; ++s) { mbar_init(smem_u32(&bars->full[s]), kFloat ? S::kRowWarps + kCodeWarps : 1 + kCodeWarps); mbar_init(smem_u32(&bars->empty[s]), 1); }
     for (int q = 0; q < kSums; ++q) { mbar_init(smem_u32(&mb->sum_full[q]), 1); mbar_init(smem_u32(&mb->sum_empty[q]), kResultWarps); }
     bars->abort_flag = 0;
     bars->wait_limit = kWaitCycles;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-    tma_prefetch_map(&xmap);
+    if (!kFloat) tma_prefetch_map(&xmap);
   }
   if (warp == 1) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;"
@@ -94,7 +98,7 @@ linear_w4_many_kernel(const __grid_constant__ CUtensorMap xmap, const LinearArgs
 
   if (warp == 0) {
     // ------------------------------------------------------------------ rows of x
-    if (lane == 0) {
+    if (!kFloat && lane == 0) {
       int stage = 0;
       uint32_t phase = 0;
       for (int p = p_first; p < p_last; ++p) {
@@ -127,8 +131,10 @@ linear_w4_many_kernel(const __grid_constant__ CUtensorMap xmap, const LinearArgs
 #pragma unroll
           for (int i = 0; i < kGroup16; ++i) {
             const int k = g * kGroup16 + i;          // of the stage's eight 16s
-            umma_bf16(tmem + buf * kCols, filters + (k >> 2) * (kFilterBytes >> 4) + 2 * (k & 3), rows + (k >> 2) * (kCols * 128 >> 4) + 2 * (k & 3), idesc,
-                      i ? 1u : 0u);
+#pragma unroll
+            for (int part = S::kParts - 1; part >= 0; --part)                // the smallest parts first
+              umma_bf16(tmem + buf * kCols, filters + (k >> 2) * (kFilterBytes >> 4) + 2 * (k & 3),
+                        rows + part * (S::kPartBytes >> 4) + (k >> 2) * (kCols * 128 >> 4) + 2 * (k & 3), idesc, i || part < S::kParts - 1 ? 1u : 0u);
           }
           umma_commit(smem_u32(&mb->sum_full[buf]));
         }
@@ -173,7 +179,7 @@ linear_w4_many_kernel(const __grid_constant__ CUtensorMap xmap, const LinearArgs
       }
     }
     const int i = filter0 + filter;
-    __nv_bfloat16* y = static_cast<__nv_bfloat16*>(a.y);
+    T* y = static_cast<T*>(a.y);
     if (splits == 1) {
       if (!bars->abort_flag && i < a.m) {
         const float bias = a.bias ? __ldg(a.bias + i) : 0.f;
@@ -181,7 +187,7 @@ linear_w4_many_kernel(const __grid_constant__ CUtensorMap xmap, const LinearArgs
         for (int q = 0; q < kMine; ++q) {
           const long long r = row0 + half * kMine + q;
           const float v = acc[q] * 64.f + bias;
-          if (r < a.rows) y[r * a.y_pitch + i] = __float2bfloat16_rn(a.relu ? relu_of(v) : v);
+          if (r < a.rows) store_value(y + r * a.y_pitch + i, a.relu ? relu_of(v) : v);
         }
       }
     } else {
@@ -197,11 +203,11 @@ linear_w4_many_kernel(const __grid_constant__ CUtensorMap xmap, const LinearArgs
           float v = 0.f;
           for (int q = 0; q < splits; ++q) v += ld_cluster_f32(mapa_shared(base + (c * 128 + filter) * 4, uint32_t(q)));
           v = v * 64.f + bias;
-          if (row0 + c < a.rows) y[(row0 + c) * a.y_pitch + i] = __float2bfloat16_rn(a.relu ? relu_of(v) : v);
+          if (row0 + c < a.rows) store_value(y + (row0 + c) * a.y_pitch + i, a.relu ? relu_of(v) : v);
         }
       }
     }
-  } else {
+  } else if (warp < 2 + kResultWarps + kCodeWarps) {
     // ------------------------------------------------------------------ codes: a tile of 16 filters for each warp
     const int w = warp - 2 - kResultWarps, g = lane >> 2, t = lane & 3;
     const int tile = min((filter0 >> 4) + w, a.n_tiles - 1);
@@ -269,6 +275,58 @@ linear_w4_many_kernel(const __grid_constant__ CUtensorMap xmap, const LinearArgs
       }
     }
   }
+  else if constexpr (kFloat) {
+    // ------------------------------------------------------------------ fp32 rows: every warp has each eighth row
+    const int w = warp - 2 - kResultWarps - kCodeWarps, g = lane >> 2, t = lane & 3, r = w * (kCols / S::kRowWarps) + g, odd = r & 1;
+    static_assert(kCols == 8 * S::kRowWarps, "a row for each four lanes");
+    const float* x = row0 + r < a.rows ? static_cast<const float*>(a.x) + (row0 + r) * a.x_pitch : nullptr;
+    // as the filters' units: the two halves of a block in the order that keeps eight lanes' 16 bytes apart
+    const uint32_t to0 = uint32_t(r) * 128 + (((t + 4 * odd) ^ (r & 7)) << 4), to1 = uint32_t(r) * 128 + (((t + 4 * (odd ^ 1)) ^ (r & 7)) << 4);
+    float4 v[2][2][2];                               // block, unit, half of it: a stage ahead
+    auto fetch = [&](int p) {
+#pragma unroll
+      for (int d = 0; d < 2; ++d)
+#pragma unroll
+        for (int n = 0; n < 2; ++n) {
+          const int k0 = p * 128 + d * 64 + (n ^ odd) * 32 + t * 8;
+          v[d][n][0] = v[d][n][1] = make_float4(0.f, 0.f, 0.f, 0.f);
+          if (!x || p >= p_last || k0 >= a.k) continue;
+          if (k0 + 8 <= a.k) {
+            v[d][n][0] = __ldg(reinterpret_cast<const float4*>(x + k0)); v[d][n][1] = __ldg(reinterpret_cast<const float4*>(x + k0 + 4));
+          } else {
+            float f[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) f[e] = k0 + e < a.k ? __ldg(x + k0 + e) : 0.f;
+            v[d][n][0] = make_float4(f[0], f[1], f[2], f[3]); v[d][n][1] = make_float4(f[4], f[5], f[6], f[7]);
+          }
+        }
+    };
+    fetch(p_first);
+    int stage = 0;
+    uint32_t phase = 0;
+    for (int p = p_first; p < p_last; ++p) {
+      if (!mbar_wait_warp(smem_u32(&bars->empty[stage]), phase ^ 1u, bars, err, 6)) break;
+      const uint32_t to = base + stage * S::kStage + S::kRowsAt;
+#pragma unroll
+      for (int d = 0; d < 2; ++d)
+#pragma unroll
+        for (int n = 0; n < 2; ++n) {
+          uint32_t part[3][4];
+          const float f[8] = {v[d][n][0].x, v[d][n][0].y, v[d][n][0].z, v[d][n][0].w, v[d][n][1].x, v[d][n][1].y, v[d][n][1].z, v[d][n][1].w};
+#pragma unroll
+          for (int e = 0; e < 4; ++e) split_pair(f[2 * e], f[2 * e + 1], part[0][e], part[1][e], part[2][e]);
+#pragma unroll
+          for (int q = 0; q < 3; ++q)
+            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + q * S::kPartBytes + d * (kCols * 128) + (n ? to1 : to0)), "r"(part[q][0]),
+                         "r"(part[q][1]), "r"(part[q][2]), "r"(part[q][3]) : "memory");
+        }
+      fetch(p + 1);
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      __syncwarp();
+      if (lane == 0) mbar_arrive(smem_u32(&bars->full[stage]));
+      if (++stage == S::kRing) { stage = 0; phase ^= 1u; }
+    }
+  }
   if (splits > 1) {
     __syncwarp();
     if (warp < 2 || warp >= 2 + kResultWarps) cluster_sync_all();
@@ -287,17 +345,18 @@ linear_w4_many_kernel(const __grid_constant__ CUtensorMap xmap, const LinearArgs
   }
 }
 
-template <int kCols>
+template <int kCols, bool kFloat>
 rt3d_status launch_many(const LinearArgs& a, const DeviceInfo& dev, cudaStream_t st) {
-  typedef ManyShape<kCols> S;
+  typedef ManyShape<kCols, kFloat> S;
   CUtensorMap xmap;
+  std::memset(&xmap, 0, sizeof(xmap));
   const cuuint64_t dims[2] = {cuuint64_t(a.k), cuuint64_t(a.rows)}, strides[1] = {cuuint64_t(a.x_pitch) * 2};
   const cuuint32_t box[2] = {64, kCols}, estr[2] = {1, 1};
-  if (encode_tiled(&xmap, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(a.x), dims, strides, box, estr, CU_TENSOR_MAP_SWIZZLE_128B) != CUDA_SUCCESS)
+  if (!kFloat && encode_tiled(&xmap, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(a.x), dims, strides, box, estr, CU_TENSOR_MAP_SWIZZLE_128B) != CUDA_SUCCESS)
     return RT3D_ERR_CUDA;
   typedef void (*Kernel)(CUtensorMap, LinearArgs, int, int32_t*);
-  static const Kernel kernels[2][3] = {{linear_w4_many_kernel<kCols, false, 1>, linear_w4_many_kernel<kCols, false, 2>, linear_w4_many_kernel<kCols, false, 3>},
-                                       {linear_w4_many_kernel<kCols, true, 1>, linear_w4_many_kernel<kCols, true, 2>, linear_w4_many_kernel<kCols, true, 3>}};
+  static const Kernel kernels[2][3] = {{linear_w4_many_kernel<kCols, kFloat, false, 1>, linear_w4_many_kernel<kCols, kFloat, false, 2>, linear_w4_many_kernel<kCols, kFloat, false, 3>},
+                                       {linear_w4_many_kernel<kCols, kFloat, true, 1>, linear_w4_many_kernel<kCols, kFloat, true, 2>, linear_w4_many_kernel<kCols, kFloat, true, 3>}};
   const int kind = a.fine ? 0 : a.group_shift + 1;
   const Kernel kernel = kernels[a.zeros != nullptr][kind];
   static std::atomic<bool> attr_done[kMaxDevices][2][3];
@@ -321,8 +380,9 @@ rt3d_status launch_many(const LinearArgs& a, const DeviceInfo& dev, cudaStream_t
 
 }  // namespace
 
-rt3d_status linear_w4_many_rows(const LinearArgs& a, const DeviceInfo& dev, cudaStream_t st) {
-  return a.rows <= 64 ? launch_many<64>(a, dev, st) : launch_many<128>(a, dev, st);
+rt3d_status linear_w4_many_rows(const LinearArgs& a, int dtype, const DeviceInfo& dev, cudaStream_t st) {
+  if (dtype == RT3D_F32) return launch_many<64, true>(a, dev, st);
+  return a.rows <= 64 ? launch_many<64, false>(a, dev, st) : launch_many<128, false>(a, dev, st);
 }
 
 }  // namespace rt3d

@@ -48,7 +48,7 @@ def test_codes_scales_and_zero_points(m, k, group, zeros, dtype, kind):
     w, codes, scales, zero = reference(wd, group, zeros)
     np.testing.assert_array_equal(q.scales.float().cpu().numpy(), w4ref.tiled(scales))
     if zeros:
-        np.testing.assert_array_equal(q.zeros.cpu().numpy(), w4ref.tiled(zero, 8))
+        np.testing.assert_array_equal(q.zeros.cpu().numpy(), w4ref.tiled(zero))
     spread = np.repeat(zero, group, 1)
     fill = np.repeat(zero[:, -1:], -(-k // 64) * 64, 1)
     fill[:, :min(fill.shape[1], spread.shape[1])] = spread[:, :fill.shape[1]]
@@ -142,6 +142,22 @@ def test_every_voxel_is_a_row():
 
 def test_many_rows():
     run_linear(5000, 48, 160, 64, True, torch.bfloat16, False, True)
+
+
+def test_more_rows_than_a_launch_takes():
+    rows, m, k = (1 << 19) + 5, 8, 64
+    wd, q = quantized(make_weights(m, k, 1), 32, True)
+    _, codes, scales, zero = reference(wd, 32, True)
+    values = torch.from_numpy(w4ref.values(codes, scales, zero, 32)).cuda()
+    for dtype in (torch.bfloat16, torch.float32):
+        x = (torch.rand(rows, 1, 1, 1, k, device="cuda") * 2 - 1).to(dtype)
+        y = torch.zeros(rows, 1, 1, 1, m, dtype=dtype, device="cuda")
+        rt3d.rt3d_linear_w4(x, q, None, y)
+        want, size = x.view(rows, k).double() @ values.t(), x.view(rows, k).abs().double() @ values.abs().t()
+        tol = w4ref.tolerance(size, k, 32)
+        if dtype == torch.bfloat16:
+            tol = tol + 2.0 ** -8 * (want.abs() + tol)
+        assert bool(((y.view(rows, m).double() - want).abs() <= tol).all())
 
 
 def test_the_same_bits_again_on_a_side_stream_and_from_a_graph():

@@ -33,7 +33,13 @@ namespace {
 
 constexpr int kNormBlocks = 512;
 constexpr int kMostSteps = 16, kRuns = kMostSteps;
-constexpr int kFusedSide = 768, kFusedLength = 1024;
+// Up to this side the small matrices' products are steps of one launch.  A side of 512 against twice the length, five steps, us: as launches 162,
+// as steps 141; 768: 169 and 166; 1024: 308 and 214; 1280: 256 either way.
+constexpr int kFusedSide = 1024;
+// Where X is short as well, everything is, with runs of one step, which need the fewest products in a row.  Side 64, us: 512 long 75 in
+// runs of three and 60 this way, 768: 75 and 71, 1024: 75 and 77; side 256: 512 100 and 83, 768 102 and 102; side 512: 1024 139 and 127,
+// 2048 142 and 154; side 768: 1536 165 and 157, three times the side 171 and 204; side 1024: 1536 211 and 209, 2048 214 and 221.
+constexpr bool everything_fused(int n, int l) { return n <= kFusedSide && (l <= 768 || (l <= 2 * n && l <= 1536)); }
 constexpr float kXScale = 16384.f, kGScale = 16384.f, kPScale = 1024.f;        // what X, G and T, P and Q are held times
 
 __device__ __forceinline__ float value_of(const float* p) { return *p; }
@@ -1020,7 +1026,7 @@ rt3d_status direction(const Source<T>& src, int m, int k, const Plan& plan, int 
   Runner r{dev, st, ws};
   if (!r.make_maps()) return RT3D_ERR_CUDA;
   const bool turned = m > k;
-  const bool short_x = (turned ? k : m) <= kFusedSide && (turned ? m : k) <= kFusedLength;
+  const bool short_x = turned ? everything_fused(k, m) : everything_fused(m, k);
   uintptr_t bits = reinterpret_cast<uintptr_t>(src.g) | uintptr_t(src.pitch) * sizeof(T);       // 4 values at a time
   bool vec = k % 4 == 0 && bits % (4 * sizeof(T)) == 0;
   if (src.momentum) vec = vec && reinterpret_cast<uintptr_t>(src.momentum) % 16 == 0 && reinterpret_cast<uintptr_t>(src.mask) % 4 == 0;
@@ -1039,8 +1045,6 @@ rt3d_status direction(const Source<T>& src, int m, int k, const Plan& plan, int 
   s = launched(vec ? cudaLaunchKernelEx(&l2.cfg, split_kernel<T, true>, src, m, k, (const double*)ws.sums, plan.eps, int(turned), x->hi, lo, x->pitch, runs, ws.factors, ws.arrived)
                    : cudaLaunchKernelEx(&l2.cfg, split_kernel<T, false>, src, m, k, (const double*)ws.sums, plan.eps, int(turned), x->hi, lo, x->pitch, runs, ws.factors, ws.arrived));
   if (s != RT3D_OK) return s;
-  // The small matrices' products are steps of one launch up to kFusedSide; where X is short as well, everything is, with runs of one
-  // step, which need the fewest products in a row.
   const int n = turned ? k : m, n_fused = n <= kFusedSide;
   int launch_no = 0;
   ProductArgs<2> one;

@@ -213,3 +213,67 @@ def test_nothing_is_launched_while_planning():
     assert rt3d.rt3d_launch_count() == before
     rt3d.rt3d_orthogonalize(g, out, ws)
     assert rt3d.rt3d_launch_count() > before and rt3d.rt3d_alloc_count() == allocs
+
+
+def test_arrays_on_odd_addresses():
+    w, momentum, g, mask = state(97, 300, True, torch.float32)
+
+    def shifted(t, by):
+        flat = torch.empty(t.numel() + by, dtype=t.dtype, device="cuda")
+        out = flat[by:].view(t.shape)
+        out.copy_(t)
+        return out
+
+    want_w, want_m, o = orthoref.update(w, momentum, g, mask, UPDATE["lr"], 0.95, True, UPDATE["weight_decay"], UPDATE["scale"])
+    step = UPDATE["lr"] * UPDATE["scale"] * o.norm()
+    for by in ((1, 0, 0, 0), (0, 1, 0, 0), (0, 0, 1, 0), (0, 0, 0, 1), (3, 2, 1, 7)):
+        wd, md, gd, kd = (shifted(t, b) for t, b in zip((w, momentum, g, mask), by))
+        rt3d.rt3d_ortho_update(wd, md, gd, kd, workspace(97, 300), **UPDATE)
+        assert (wd.double().cpu() - want_w).norm() <= 1e-4 * step + 2.0 ** -22 * (w.double().norm() + step)
+        assert (md.double().cpu() - want_m).norm() <= 2.0 ** -23 * (momentum.double().norm() + g.double().norm())
+
+
+@pytest.mark.parametrize("m,k", [(3, 50000), (50000, 3), (130, 20000), (900, 1100), (1024, 1500), (1030, 1040)])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_long_and_middling_matrices(m, k, dtype):
+    gen = torch.Generator(device="cuda").manual_seed(m)
+    g = (torch.randn(m, k, generator=gen, device="cuda") * 1e-3).to(dtype)
+    assert off(orthogonalize(g), orthoref.direction(g)) <= 2.0 ** -8 + 3e-3
+
+
+def test_two_calls_at_once():
+    """Two streams with a workspace each: steps that wait for one another inside a launch, a cluster's and a grid's."""
+    for m, k in ((144, 576), (512, 2048), (700, 900)):
+        states = [[t.cuda() for t in state(m, k, True, torch.float32, seed)] for seed in (1, 2)]
+        alone = []
+        for w, momentum, g, mask in states:
+            a, b = w.clone(), momentum.clone()
+            for _ in range(4):
+                rt3d.rt3d_ortho_update(a, b, g, mask, workspace(m, k), **UPDATE)
+            alone.append((a, b))
+        torch.cuda.synchronize()
+        streams, spaces = [torch.cuda.Stream() for _ in states], [workspace(m, k) for _ in states]
+        together = [(w.clone(), momentum.clone()) for w, momentum, _, _ in states]
+        torch.cuda.synchronize()
+        for _ in range(4):
+            for st, ws, (a, b), (_, _, g, mask) in zip(streams, spaces, together, states):
+                with torch.cuda.stream(st):
+                    rt3d.rt3d_ortho_update(a, b, g, mask, ws, **UPDATE)
+        torch.cuda.synchronize()
+        assert rt3d.rt3d_last_device_status() == rt3d.OK
+        assert all(torch.equal(p, q) for x, y in zip(alone, together) for p, q in zip(x, y))
+
+
+def test_rows_that_share_memory_are_refused():
+    row = torch.randn(1, 64, device="cuda")
+    with pytest.raises(rt3d.Rt3dError):
+        rt3d.rt3d_orthogonalize(row.expand(32, 64), torch.empty(32, 64, dtype=torch.bfloat16, device="cuda"), workspace(32, 64))
+    with pytest.raises(ValueError):
+        rt3d.rt3d_orthogonalize(torch.randn(64, 32, device="cuda").t(), torch.empty(32, 64, dtype=torch.bfloat16, device="cuda"), workspace(32, 64))
+
+
+def test_poisoned_shared_memory():
+    for m, k in ((20, 100), (144, 576), (300, 3000)):
+        g = (orthoref.matrix("falling", m, k, 3) * 1e-3).to(torch.bfloat16)
+        rt3d.rt3d_debug_set(rt3d.DEBUG_POISON, 0x7FC07FC0)
+        assert off(orthogonalize(g.cuda()), orthoref.direction(g)) <= 2.0 ** -8 + 3e-3

@@ -202,3 +202,47 @@ def test_nothing_is_allocated_or_launched_while_planning():
     assert rt3d.rt3d_launch_count() == before
     rt3d.rt3d_linear_w4(rt3d.tensor_desc(x, q.k), q, b, rt3d.tensor_desc(y, q.m))
     assert rt3d.rt3d_launch_count() > before and rt3d.rt3d_alloc_count() == allocs
+
+
+@pytest.mark.parametrize("rows", [2, 20])
+def test_codes_past_32_bits(rows):
+    """5.2 billion weights, 2.6 GB of codes: the last tile's filters against the same tile on its own, in 64 bits."""
+    m, k, group = 40000, 131072, 64
+    q = rt3d.W4Weights(m, k, group, zeros=True)
+    q.codes.view(torch.int64).random_()
+    q.scales.copy_(torch.rand(q.scales.shape, device="cuda") * 0.01)
+    q.zeros.copy_(torch.randint(0, 16, q.zeros.shape, device="cuda"))
+    x = (torch.rand(rows, 1, 1, 1, k, device="cuda") * 2 - 1).to(torch.bfloat16)
+    y = torch.zeros(rows, 1, 1, 1, m, dtype=torch.bfloat16, device="cuda")
+    rt3d.rt3d_linear_w4(x, q, None, y)
+    last = rt3d.W4Weights(16, k, group, codes=q.codes[-16 * k // 2:].clone(), scales=q.scales[-1:].clone(), zeros=q.zeros[-1:].clone())
+    values = torch.empty(16, k, device="cuda")
+    rt3d.rt3d_w4_unpack(last, values)
+    xs = x.view(rows, k).double()
+    want, size = xs @ values.double().t(), xs.abs() @ values.double().abs().t()
+    tol = w4ref.tolerance(size, k, group)
+    tol = tol + 2.0 ** -8 * (want.abs() + tol)
+    assert bool(((y.view(rows, m)[:, -16:].double() - want).abs() <= tol).all())
+
+
+def test_two_streams_at_once():
+    parts = [run_linear(rows, 300, 4096, 64, True, torch.bfloat16, True, True, seed=rows) for rows in (3, 70)]
+    want = [p[3].clone() for p in parts]
+    streams = [torch.cuda.Stream() for _ in parts]
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for st, (x, q, b, y) in zip(streams, parts):
+            with torch.cuda.stream(st):
+                rt3d.rt3d_linear_w4(rt3d.tensor_desc(x, q.k), q, b, rt3d.tensor_desc(y, q.m), relu=True)
+    torch.cuda.synchronize()
+    assert rt3d.rt3d_last_device_status() == rt3d.OK
+    assert all(torch.equal(p[3], w) for p, w in zip(parts, want))
+
+
+def test_shared_and_poisoned_memory():
+    """Products after every SM's shared and tensor memory has been filled with NaNs."""
+    for rows, dtype in ((1, torch.bfloat16), (12, torch.float32), (40, torch.bfloat16), (100, torch.bfloat16), (40, torch.float32)):
+        rt3d.rt3d_debug_set(rt3d.DEBUG_POISON, 0x7FC07FC0)
+        run_linear(rows, 45, 200, 32, True, dtype, False, True)
+        rt3d.rt3d_debug_set(rt3d.DEBUG_POISON, 0x7FC07FC0)
+        run_linear(rows, 200, 130, 128, False, dtype, False, True)

@@ -74,50 +74,80 @@ __device__ __forceinline__ void load4(const T* p, int n, float (&v)[4]) {
     for (int e = 0; e < 4; ++e) v[e] = e < n ? value_of(p + e) : 0.f;
   }
 }
-template <typename T, bool kFirst, bool kVec>
-__device__ __forceinline__ void source4(const Source<T>& s, int i, int j, int k, float (&v)[4]) {
-  const int n = k - j;
-  load4<T, kVec>(s.g + (long long)i * s.pitch + j, n, v);
-  if (!s.momentum) return;
-  const long long at = (long long)i * k + j;
-  uint32_t keep = 0x01010101u;
-  if (s.mask) {
-    if (kVec) keep = *reinterpret_cast<const uint32_t*>(s.mask + at);
-    else {
+// Four neighbours of the source: what they are made of, loaded, and then the values; the first kernel writes the momentum.
+template <typename T, bool kVec>
+struct Quad {
+  float g[4], m[4];
+  uint32_t keep;
+  __device__ __forceinline__ void load(const Source<T>& s, long long g_at, long long at, int n) {
+    load4<T, kVec>(s.g + g_at, n, g);
+    keep = 0x01010101u;
+    if (!s.momentum) return;
+    load4<float, kVec>(s.momentum + at, n, m);
+    if (!s.mask) return;
+    if constexpr (kVec) {
+      keep = *reinterpret_cast<const uint32_t*>(s.mask + at);
+    } else {
       keep = 0;
       for (int e = 0; e < 4 && e < n; ++e) keep |= uint32_t(s.mask[at + e]) << (8 * e);
     }
   }
-  float m[4];
-  load4<float, kVec>(s.momentum + at, n, m);
+  template <bool kFirst>
+  __device__ __forceinline__ void values(const Source<T>& s, long long at, int n, float (&v)[4]) {
 #pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    const bool on = (keep >> (8 * e)) & 0xffu;
-    if (kFirst) m[e] = on ? fmaf(s.mu, m[e], v[e]) : 0.f;
-    v[e] = !on ? 0.f : s.nesterov ? fmaf(s.mu, m[e], v[e]) : m[e];
+    for (int e = 0; e < 4; ++e) v[e] = g[e];
+    if (!s.momentum) return;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const bool on = (keep >> (8 * e)) & 0xffu;
+      if (kFirst) m[e] = on ? fmaf(s.mu, m[e], v[e]) : 0.f;
+      v[e] = !on ? 0.f : s.nesterov ? fmaf(s.mu, m[e], v[e]) : m[e];
+    }
+    if (kFirst) {
+      if constexpr (kVec) *reinterpret_cast<float4*>(s.momentum + at) = make_float4(m[0], m[1], m[2], m[3]);
+      else
+        for (int e = 0; e < 4 && e < n; ++e) s.momentum[at + e] = m[e];
+    }
   }
-  if (kFirst) {
-    if (kVec) *reinterpret_cast<float4*>(s.momentum + at) = make_float4(m[0], m[1], m[2], m[3]);
-    else
-      for (int e = 0; e < 4 && e < n; ++e) s.momentum[at + e] = m[e];
-  }
-}
+};
 
-// Sums of squares of the blocks' shares, in 64 bits: neither overflow nor the order of a long sum matters.
-template <typename T, bool kVec>
+// Sums of squares of the blocks' shares, in 64 bits: neither overflow nor the order of a long sum matters.  Four quads of a thread are
+// on their way at a time; kFlat: rows without gaps, whose places need no division.
+template <typename T, bool kVec, bool kFlat>
 __global__ void __launch_bounds__(256)
 square_sums_kernel(Source<T> s, int m, int k, double* __restrict__ sums) {
   pdl_entry();
   __shared__ double part[8];
   const unsigned quads = unsigned(k + 3) / 4;
-  const unsigned long long total = (unsigned long long)m * quads;
+  const long long total = kFlat ? (long long)m * k / 4 : (long long)m * quads;
+  constexpr long long kStep = (long long)kNormBlocks * 256;
   double sum = 0.0;
-  for (unsigned long long idx = blockIdx.x * 256u + threadIdx.x; idx < total; idx += kNormBlocks * 256u) {
-    const int i = total >> 32 ? int(idx / quads) : int(unsigned(idx) / quads);
-    float v[4];
-    source4<T, true, kVec>(s, i, int(idx - (unsigned long long)i * quads) * 4, k, v);
+  for (long long first = blockIdx.x * 256 + threadIdx.x; first < total; first += 4 * kStep) {
+    Quad<T, kVec> quad[4];
+    long long at[4];
+    int n[4];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) sum += double(v[e]) * v[e];
+    for (int q = 0; q < 4; ++q) {
+      const long long idx = first + q * kStep;
+      n[q] = 0;
+      if (idx >= total) continue;
+      if (kFlat) {
+        at[q] = idx * 4; n[q] = 4;
+        quad[q].load(s, at[q], at[q], 4);
+      } else {
+        const int i = total >> 32 ? int(idx / quads) : int(unsigned(idx) / quads), j = int(idx - (long long)i * quads) * 4;
+        at[q] = (long long)i * k + j; n[q] = k - j;
+        quad[q].load(s, (long long)i * s.pitch + j, at[q], n[q]);
+      }
+    }
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      if (n[q] == 0) continue;
+      float v[4];
+      quad[q].template values<true>(s, at[q], n[q], v);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) sum += double(v[e]) * v[e];
+    }
   }
   for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
   if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = sum;
@@ -161,30 +191,43 @@ split_kernel(Source<T> s, int m, int k, const double* __restrict__ sums, double 
   pdl_entry();
   __shared__ double part[8];
   __shared__ float tile[32][133];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int cols = (k + 127) / 128;
+  const int i0 = int(blockIdx.x / cols) * 32, j0 = int(blockIdx.x % cols) * 128, j = j0 + lane * 4;
+  Quad<T, kVec> quad[4];                                         // on their way while the norm is worked out
+#pragma unroll
+  for (int p = 0; p < 4; ++p) {
+    const int i = i0 + p * 8 + warp;
+    if (i < m && j < k) quad[p].load(s, (long long)i * s.pitch + j, (long long)i * k + j, k - j);
+  }
   double sum = sums[threadIdx.x] + sums[threadIdx.x + 256];
   for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
   if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = sum;
   __syncthreads();
-  sum = part[0];
-  for (int w = 1; w < 8; ++w) sum += part[w];
+  __shared__ float scale_s[2];                                   // powers of two, whose product may leave the range of 32 bits
   if (blockIdx.x == 0 && threadIdx.x < kRuns) arrived[threadIdx.x] = 0;
-  const double norm = sqrt(sum);
-  const bool number = norm > 0.0 && norm < 1e300;                // one that is none makes everything NaN
-  const double power = number ? exp2(floor(-log2(norm))) : 1.0;
-  if (blockIdx.x == 0 && threadIdx.x == 0)
-    write_factors(number ? 1.0 / ((norm + eps) * power) : norm == 0.0 ? 1.0 : __longlong_as_double(0x7fffffffffffffffll), runs, factors);
-  const double scale = power * kXScale;
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int cols = (k + 127) / 128;
-  const int i0 = int(blockIdx.x / cols) * 32, j0 = int(blockIdx.x % cols) * 128;
+  if (threadIdx.x == 0) {                                        // one thread: 64-bit roots and exponents are slow
+    sum = part[0];
+    for (int w = 1; w < 8; ++w) sum += part[w];
+    const double norm = sqrt(sum);
+    const bool number = norm > 0.0 && norm < 1e300;              // one that is none makes everything NaN
+    const int e = number ? -ilogb(norm) - 1 : 0, up = e + 14, first = up / 2;  // norm * 2^e in [1/2, 1)
+    const double power = scalbn(1.0, e);
+    scale_s[0] = scalbnf(1.f, first); scale_s[1] = scalbnf(1.f, up - first);
+    if (blockIdx.x == 0)
+      write_factors(number ? 1.0 / ((norm + eps) * power) : norm == 0.0 ? 1.0 : __longlong_as_double(0x7fffffffffffffffll), runs, factors);
+  }
+  __syncthreads();
+  const float scale0 = scale_s[0], scale1 = scale_s[1];
+  static_assert(kXScale == 16384.f, "2^14");
 #pragma unroll
   for (int p = 0; p < 4; ++p) {
-    const int r = p * 8 + warp, i = i0 + r, j = j0 + lane * 4;
+    const int r = p * 8 + warp, i = i0 + r;
     if (i >= m || j >= k) continue;
     float v[4];
-    source4<T, false, kVec>(s, i, j, k, v);
+    quad[p].template values<false>(s, 0, 0, v);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = float(v[e] * scale);
+    for (int e = 0; e < 4; ++e) v[e] = v[e] * scale0 * scale1;
     if (turned) {
 #pragma unroll
       for (int e = 0; e < 4; ++e) tile[r][lane * 4 + e] = v[e];
@@ -1031,8 +1074,9 @@ rt3d_status direction(const Source<T>& src, int m, int k, const Plan& plan, int 
   bool vec = k % 4 == 0 && bits % (4 * sizeof(T)) == 0;
   if (src.momentum) vec = vec && reinterpret_cast<uintptr_t>(src.momentum) % 16 == 0 && reinterpret_cast<uintptr_t>(src.mask) % 4 == 0;
   LaunchSetup l1(dim3(kNormBlocks), dim3(256), 0, st);
-  rt3d_status s = launched(vec ? cudaLaunchKernelEx(&l1.cfg, square_sums_kernel<T, true>, src, m, k, ws.sums)
-                               : cudaLaunchKernelEx(&l1.cfg, square_sums_kernel<T, false>, src, m, k, ws.sums));
+  rt3d_status s = launched(vec && src.pitch == k ? cudaLaunchKernelEx(&l1.cfg, square_sums_kernel<T, true, true>, src, m, k, ws.sums)
+                           : vec                 ? cudaLaunchKernelEx(&l1.cfg, square_sums_kernel<T, true, false>, src, m, k, ws.sums)
+                                                 : cudaLaunchKernelEx(&l1.cfg, square_sums_kernel<T, false, false>, src, m, k, ws.sums));
   if (s != RT3D_OK) return s;
   const Matrix* x = &ws.all[kX0];
   int parts = !exact && sizeof(T) == 2 ? 1 : 2;

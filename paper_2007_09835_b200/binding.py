@@ -152,7 +152,8 @@ _lib = _load()
 
 ADDRESS = {fn: ctypes.cast(getattr(_lib, fn), ctypes.c_void_p).value
            for fn in ("rt3d_conv3d_sparse", "rt3d_conv3d_dense", "rt3d_conv3d_sparse_fused", "rt3d_kgs_group_norms",
-                      "rt3d_kgs_reweight", "rt3d_kgs_expand_mask", "rt3d_linear_w4")}
+                      "rt3d_kgs_reweight", "rt3d_kgs_expand_mask", "rt3d_linear_w4", "rt3d_w4_quantize",
+                      "rt3d_w4_unpack")}
 _pycall_module = None
 
 
@@ -639,14 +640,12 @@ class W4Weights:
 
 def rt3d_w4_quantize(w, q: W4Weights, stream=None):
     """w: device tensor [m][k] or [m][N][Kt][Kh][Kw], float32 or bfloat16, rows contiguous (any row pitch); fills q."""
-    ptr, dtype, pitch = _matrix(w, q.m, q.k)
-    _check(_lib.rt3d_w4_quantize(ptr, dtype, pitch, ctypes.byref(q.desc), _stream_ptr(stream)), "rt3d_w4_quantize")
+    _check((_pycall_module or pycall()).w4_quantize(ADDRESS["rt3d_w4_quantize"], q.desc, w, stream), "rt3d_w4_quantize")
 
 
 def rt3d_w4_unpack(q: W4Weights, w, stream=None):
     """w: device tensor as for rt3d_w4_quantize (output): the values that the codes stand for."""
-    ptr, dtype, pitch = _matrix(w, q.m, q.k)
-    _check(_lib.rt3d_w4_unpack(ctypes.byref(q.desc), dtype, ptr, pitch, _stream_ptr(stream)), "rt3d_w4_unpack")
+    _check((_pycall_module or pycall()).w4_unpack(ADDRESS["rt3d_w4_unpack"], q.desc, w, stream), "rt3d_w4_unpack")
 
 
 def rt3d_linear_w4(x, q: W4Weights, bias, y, relu=False, stream=None):

@@ -272,6 +272,60 @@ PyObject* linear_w4(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+// The rows of a matrix as binding._matrix describes them, with the same refusals.
+bool matrix(PyObject* t, int64_t m, int64_t k, uintptr_t* data, int* dtype, int64_t* pitch) {
+  PyObject* shape = PyObject_GetAttr(t, s_shape);
+  if (!shape) return false;
+  PyObject* st = PyObject_CallMethodNoArgs(t, s_stride);
+  bool ok = st && PyTuple_Check(shape) && PyTuple_Check(st) && PyTuple_GET_SIZE(shape) >= 2 && PyTuple_GET_SIZE(st) == PyTuple_GET_SIZE(shape);
+  int64_t want = 1, first = 0;
+  if (ok) {
+    for (Py_ssize_t i = PyTuple_GET_SIZE(shape) - 1; i > 0 && ok; --i) {
+      const int64_t e = PyLong_AsLongLong(PyTuple_GET_ITEM(shape, i));
+      ok = e == 1 || PyLong_AsLongLong(PyTuple_GET_ITEM(st, i)) == want;
+      want *= e;
+    }
+    first = PyLong_AsLongLong(PyTuple_GET_ITEM(st, 0));
+    ok = ok && want == k && PyLong_AsLongLong(PyTuple_GET_ITEM(shape, 0)) == m;
+  }
+  Py_DECREF(shape);
+  Py_XDECREF(st);
+  if (PyErr_Occurred()) return false;
+  if (!ok) {
+    PyErr_Format(PyExc_ValueError, "expected %lld contiguous rows of %lld values", (long long)m, (long long)k);
+    return false;
+  }
+  *pitch = m > 1 || first > k ? first : k;
+  PyObject* dt = PyObject_GetAttr(t, s_dtype);
+  if (!dt) return false;
+  *dtype = dt == g_float32 ? RT3D_F32 : dt == g_bfloat16 ? RT3D_BF16 : -1;
+  if (*dtype < 0) PyErr_Format(PyExc_ValueError, "expected float32 or bfloat16, got %S", dt);
+  Py_DECREF(dt);
+  return *dtype >= 0 && data_ptr(t, data);
+}
+
+// w4_quantize(address, weights, w, stream) and w4_unpack(address, weights, w, stream) -> status
+PyObject* w4_quantize(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  uintptr_t fn, w, stream;
+  rt3d_w4 q;
+  int dtype;
+  int64_t pitch;
+  if (!want(n, 4) || !as_pointer(a[0], &fn) || !structure(a[1], &q) || !matrix(a[2], q.m, q.k, &w, &dtype, &pitch) || !stream_of(a[3], &stream)) return nullptr;
+  return released([&] {
+    return reinterpret_cast<decltype(&rt3d_w4_quantize)>(fn)(reinterpret_cast<const void*>(w), dtype, pitch, &q, reinterpret_cast<void*>(stream));
+  });
+}
+PyObject* w4_unpack(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  uintptr_t fn, w, stream;
+  rt3d_w4 q;
+  int dtype;
+  int64_t pitch;
+  if (!want(n, 4) || !as_pointer(a[0], &fn) || !structure(a[1], &q) || !matrix(a[2], q.m, q.k, &w, &dtype, &pitch) || !stream_of(a[3], &stream)) return nullptr;
+  return released([&] {
+    return reinterpret_cast<decltype(&rt3d_w4_unpack)>(fn)(&q, dtype, reinterpret_cast<void*>(w), pitch, reinterpret_cast<void*>(stream));
+  });
+}
+
 PyMethodDef methods[] = {
     {"setup", setup, METH_VARARGS, "setup(float32, bfloat16, raw_stream, get_device): torch objects the calls need"},
     {"conv", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(conv)), METH_FASTCALL,
@@ -281,6 +335,8 @@ PyMethodDef methods[] = {
     {"expand_mask", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(expand_mask)), METH_FASTCALL, ""},
     {"linear_w4", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(linear_w4)), METH_FASTCALL,
      "linear_w4(address, x, weights, bias, y, relu, stream) -> status"},
+    {"w4_quantize", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(w4_quantize)), METH_FASTCALL, ""},
+    {"w4_unpack", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(w4_unpack)), METH_FASTCALL, ""},
     {"pointers_are", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(pointers_are)), METH_FASTCALL,
      "pointers_are(tensors, addresses) -> bool"},
     {nullptr, nullptr, 0, nullptr}};

@@ -246,3 +246,17 @@ def test_shared_and_poisoned_memory():
         run_linear(rows, 45, 200, 32, True, dtype, False, True)
         rt3d.rt3d_debug_set(rt3d.DEBUG_POISON, 0x7FC07FC0)
         run_linear(rows, 200, 130, 128, False, dtype, False, True)
+
+
+def test_matrices_that_are_refused():
+    q = rt3d.W4Weights(40, 200, 32)
+    for w in (torch.zeros(40, 199, device="cuda"), torch.zeros(39, 200, device="cuda"), torch.zeros(200, 40, device="cuda").t(), torch.zeros(8000, device="cuda"),
+              torch.zeros(40, 200, device="cuda", dtype=torch.float16), torch.zeros(40, 400, device="cuda")[:, ::2], torch.zeros(40, 8, 1, 5, 6, device="cuda")):
+        for call in (lambda: rt3d.rt3d_w4_quantize(w, q), lambda: rt3d.rt3d_w4_unpack(q, w)):
+            with pytest.raises(ValueError):
+                call()
+    with pytest.raises(rt3d.Rt3dError) as e:
+        rt3d.rt3d_w4_quantize(torch.zeros(1, 200, device="cuda").expand(40, 200), q)         # rows that share memory
+    assert e.value.status == rt3d.ERR_INVALID_ARG
+    with pytest.raises((TypeError, AttributeError, ValueError)):
+        rt3d.rt3d_w4_quantize(np.zeros((40, 200), np.float32), q)

@@ -1018,20 +1018,40 @@ struct Fused {
   }
   Problem* add() { return &a.steps.p[n_problems++]; }
   void end_step() { a.steps.first[++a.n_steps] = n_problems; }
+  // CTAs of a cluster that the device places: 16, or the 8 that every one does.
+  static int most_of_cluster() {
+    static std::atomic<int> known[kMaxDevices];
+    const int d = current_device_index();
+    if (d < 0) return 8;
+    int v = known[d].load();
+    if (v == 0) {
+      const auto kernel = product_kernel<64, kMostProblems>;
+      int n = 0;
+      LaunchSetup ls(dim3(16), dim3(kProductThreads), kProductSmem<64>, nullptr, 16);
+      ls.cfg.numAttrs = 1;                                       // the cluster dimension alone
+      v = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(kProductSmem<64>)) == cudaSuccess &&
+                  cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) == cudaSuccess &&
+                  cudaOccupancyMaxActiveClusters(&n, kernel, &ls.cfg) == cudaSuccess && n > 0 ? 16 : 8;
+      if (v == 8) cudaGetLastError();
+      known[d].store(v);
+    }
+    return v;
+  }
   // A cluster's wait takes 0.5 us, a grid's 1.5: eight CTAs where going round more often than a grid would costs less than that
   // (a chunk of three products of 128 x 64: 700 clocks).
   rt3d_status run(unsigned* arrived) {
+    const int side = most_of_cluster();
     int most = 1, extra = 0;
     for (int s = 0; s < a.n_steps; ++s) {
       int items = 0;
       for (int p = a.steps.first[s]; p < a.steps.first[s + 1]; ++p) items += a.steps.p[p].n_tiles;
       most = items > most ? items : most;
-      extra += (ceil_div(items, 8) - ceil_div(items, r.dev.sm_count)) * a.steps.p[a.steps.first[s]].chunks;
+      extra += (ceil_div(items, side) - ceil_div(items, r.dev.sm_count)) * a.steps.p[a.steps.first[s]].chunks;
     }
     a.splits = 1;
     a.one_cluster = extra * 700 <= a.n_steps * 1900;
     a.arrived = arrived;
-    const int grid = a.one_cluster ? (most < 8 ? most : 8) : most < r.dev.sm_count ? most : r.dev.sm_count;
+    const int grid = a.one_cluster ? (most < side ? most : side) : most < r.dev.sm_count ? most : r.dev.sm_count;
     return r.launch<64>(a, grid, a.one_cluster ? unsigned(grid) : 1u, !a.one_cluster && a.n_steps > 1);
   }
 };

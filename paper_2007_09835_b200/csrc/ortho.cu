@@ -265,6 +265,7 @@ constexpr int kTile = 128;                           // rows of a tile
 constexpr uint32_t kRowsBytes = kTile * 128;         // of 128 x 64 fp16
 constexpr int kProductThreads = 320;                 // producer, issuer, eight warps for the results
 constexpr int kMostProblems = 16;                    // of one launch
+constexpr int kMostCluster = 16;
 
 // Tiles of 128 x kCols: a stage holds 64 of the sum of up to four operands (hi and lo of A and B), as many as the launch's products have.
 template <int kCols>
@@ -966,6 +967,30 @@ struct Runner {
     p->rows = m.rows; p->cols = m.cols;
   }
 
+  // Clusters of `size` CTAs (up to 16, where 8 are portable) that the device holds at once.
+  template <int kCols, int kProblems>
+  static int clusters_at_once(int size) {
+    static std::atomic<int> known[kMaxDevices][kMostCluster + 1];             // and one
+    const int d = current_device_index();
+    if (d < 0) return 0;
+    int v = known[d][size].load();
+    if (v == 0) {
+      const auto kernel = product_kernel<kCols, kProblems>;
+      int n = 0;
+      LaunchSetup ls(dim3(unsigned(size)), dim3(kProductThreads), kProductSmem<kCols>, nullptr, unsigned(size));
+      ls.cfg.numAttrs = 1;                                       // the cluster dimension alone
+      if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(kProductSmem<kCols>)) != cudaSuccess ||
+          cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess ||
+          cudaOccupancyMaxActiveClusters(&n, kernel, &ls.cfg) != cudaSuccess) {
+        cudaGetLastError();
+        n = 0;
+      }
+      v = n + 1;
+      known[d][size].store(v);
+    }
+    return v - 1;
+  }
+
   template <int kCols, int kProblems>
   rt3d_status launch(ProductArgs<kProblems>& a, int grid, unsigned cluster, bool cooperative) const {
     const auto kernel = product_kernel<kCols, kProblems>;
@@ -1000,8 +1025,11 @@ struct Runner {
     int items = 0;
     for (int i = 0; i < n_problems; ++i) items += a.steps.p[i].n_tiles;
     a.steps.first[0] = 0; a.steps.first[1] = n_problems; a.n_steps = 1;
+    // the largest cluster of which the device holds one for every tile, two chunks and more to a CTA
     a.splits = 1;
-    while (a.splits < 8 && items * a.splits * 2 <= dev.sm_count && a.steps.p[0].chunks >= 2 * a.splits) a.splits *= 2;
+    if (2 * items <= dev.sm_count)
+      for (int s = kMostCluster; s > 1 && a.splits == 1; --s)
+        if (items * s <= dev.sm_count && a.steps.p[0].chunks >= 2 * s && clusters_at_once<kTile, 2>(s) >= items) a.splits = s;
     return launch<kTile>(a, a.splits > 1 ? items * a.splits : items < dev.sm_count ? items : dev.sm_count, unsigned(a.splits), false);
   }
 };
@@ -1018,29 +1046,10 @@ struct Fused {
   }
   Problem* add() { return &a.steps.p[n_problems++]; }
   void end_step() { a.steps.first[++a.n_steps] = n_problems; }
-  // CTAs of a cluster that the device places: 16, or the 8 that every one does.
-  static int most_of_cluster() {
-    static std::atomic<int> known[kMaxDevices];
-    const int d = current_device_index();
-    if (d < 0) return 8;
-    int v = known[d].load();
-    if (v == 0) {
-      const auto kernel = product_kernel<64, kMostProblems>;
-      int n = 0;
-      LaunchSetup ls(dim3(16), dim3(kProductThreads), kProductSmem<64>, nullptr, 16);
-      ls.cfg.numAttrs = 1;                                       // the cluster dimension alone
-      v = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(kProductSmem<64>)) == cudaSuccess &&
-                  cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) == cudaSuccess &&
-                  cudaOccupancyMaxActiveClusters(&n, kernel, &ls.cfg) == cudaSuccess && n > 0 ? 16 : 8;
-      if (v == 8) cudaGetLastError();
-      known[d].store(v);
-    }
-    return v;
-  }
-  // A cluster's wait takes 0.5 us, a grid's 1.5: eight CTAs where going round more often than a grid would costs less than that
+  // A cluster's wait takes 0.5 us, a grid's 1.5: a cluster's CTAs where going round more often than a grid would costs less than that
   // (a chunk of three products of 128 x 64: 700 clocks).
   rt3d_status run(unsigned* arrived) {
-    const int side = most_of_cluster();
+    const int side = Runner::clusters_at_once<64, kMostProblems>(kMostCluster) > 0 ? kMostCluster : 8;
     int most = 1, extra = 0;
     for (int s = 0; s < a.n_steps; ++s) {
       int items = 0;

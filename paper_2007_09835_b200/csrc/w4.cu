@@ -20,7 +20,6 @@ __device__ __forceinline__ uint32_t cluster_size() {
   return r;
 }
 
-
 __device__ __forceinline__ int shift_of(int e) { return 4 * ((e >> 1) + 4 * (e & 1)); }
 
 // Scale, zero point and codes of a group as include/rt3d.h defines them.
@@ -260,7 +259,9 @@ w4_unpack_kernel(T* __restrict__ w, const GridArgs a) {
 // share the inputs further and add their sums up through one another's shared memory, always in the same order.
 constexpr int kLinearThreads = 256;
 constexpr int kMostRows = 1 << 19;                          // of a launch
-constexpr int kManyRows = 16;                               // more go to linear_w4_many_rows
+// More rows go to linear_w4_many_rows.  4096 x 8192, us: 16 bf16 rows 11.2 here and 14 there, 32 rows 20 and 14; 16 fp32 rows 34 and 35.5, 64
+// rows 126 and 37.
+constexpr int kManyRows = 16;
 
 __device__ __forceinline__ void mma_bf16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
   asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
@@ -578,13 +579,15 @@ linear_w4_kernel(const LinearArgs a) {
 }
 
 bool valid_extents(int64_t m, int64_t k) { return m > 0 && k > 0; }
+// Tiles of codes are counted, and inputs addressed, in 32 bits.
+bool small_enough(int64_t m, int64_t k) { return k <= (1 << 30) && ceil_div64(m, 16) * ceil_div64(k, 64) < (int64_t(1) << 31); }
 bool valid_group(int group) { return group == 32 || group == 64 || group == 128; }
 
 rt3d_status check_w4(const rt3d_w4* q) {
   if (!q || !q->codes || !q->scales || !valid_extents(q->m, q->k) || !valid_group(q->group)) return RT3D_ERR_INVALID_ARG;
   const uintptr_t bits = reinterpret_cast<uintptr_t>(q->codes) | reinterpret_cast<uintptr_t>(q->scales) | reinterpret_cast<uintptr_t>(q->zeros);
   if (bits & 15) return RT3D_ERR_INVALID_ARG;
-  if (ceil_div64(q->m, 16) * ceil_div64(q->k, 64) >= (int64_t(1) << 31)) return RT3D_ERR_UNSUPPORTED;
+  if (!small_enough(q->m, q->k)) return RT3D_ERR_UNSUPPORTED;
   return RT3D_OK;
 }
 // Arguments of the calls that read or write a plain matrix.
@@ -702,7 +705,7 @@ using namespace rt3d;
 extern "C" {
 
 int64_t rt3d_w4_codes_bytes(int m, int k) {
-  if (!valid_extents(m, k) || ceil_div64(m, 16) * ceil_div64(k, 64) >= (int64_t(1) << 31)) return -1;
+  if (!valid_extents(m, k) || !small_enough(m, k)) return -1;
   return ceil_div64(m, 16) * ceil_div64(k, 64) * 512;
 }
 

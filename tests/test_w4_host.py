@@ -18,7 +18,7 @@ def test_sizes():
     assert B.rt3d_w4_codes_bytes(4096, 8192) == 4096 * 8192 // 2
     assert B.rt3d_w4_scale_count(17, 65, 32) == 32 * 3
     assert B.rt3d_w4_scale_count(16, 128, 128) == 16
-    for m, k in ((0, 64), (16, 0), (-1, 64), (2 ** 31 - 1, 2 ** 31 - 1)):
+    for m, k in ((0, 64), (16, 0), (-1, 64), (2 ** 31 - 1, 2 ** 31 - 1), (1, 2 ** 30 + 1)):
         assert B.rt3d_w4_codes_bytes(m, k) == -1 and B.rt3d_w4_scale_count(m, k, 32) == -1
     for group in (0, 16, 48, 256, -32):
         assert B.rt3d_w4_scale_count(16, 64, group) == -1

@@ -278,6 +278,7 @@ __device__ __forceinline__ void copy16_part(uint32_t dst, const void* src, int b
 __device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int kPending>
 __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(kPending) : "memory"); }
+
 // Eight inputs of a row as bf16 pairs, 512 bytes between a lane's units.
 template <typename T>
 struct Operand;
@@ -301,7 +302,6 @@ struct Operand<float> {
     }
   }
 };
-
 
 // A stage of a warp's ring: kDeep neighbouring blocks of 64 inputs: the codes [block][tile], the rows of x [block], then the
 // groups' scales [tile][group] and zero points.

@@ -47,6 +47,15 @@ def to_numpy(t: torch.Tensor, c: int) -> np.ndarray:
     return t[..., :c].float().cpu().numpy()
 
 
+def _on(stream, device):
+    """Context whose torch work is enqueued on the stream (a handle) that a call was given; None: the current one.  What a call
+    makes for itself (copies, zeroed outputs) has to be in the order of the kernel that uses it, and its memory in that stream's pool."""
+    if stream is None:
+        return contextlib.nullcontext()
+    # an ExternalStream of the handle 0 would be a stream of its own
+    return torch.cuda.stream(torch.cuda.ExternalStream(int(stream), device) if int(stream) else torch.cuda.default_stream(device))
+
+
 # The last assignment to any layer's attribute, a value of its own for each: a noted sequence of calls holds from one to the next.
 _changes, _layer_changes = itertools.count(1), 0
 
@@ -156,7 +165,8 @@ class LinearW4Layer:
         """New weights into the layer's codes and scales."""
         if not isinstance(w, torch.Tensor):
             w = torch.from_numpy(np.ascontiguousarray(w, np.float32))
-        B.rt3d_w4_quantize(w.to(self.device), self.weights, stream)
+        with _on(stream, self.device):              # a copy of the weights lives in the order of the kernel that reads it
+            B.rt3d_w4_quantize(w.to(self.device), self.weights, stream)
 
     def out_shape(self, x: torch.Tensor):
         return tuple(x.shape[:4]) + (pitch_for(self.spec.cout, self.dtype),)

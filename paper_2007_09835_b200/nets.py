@@ -99,7 +99,8 @@ class ConvLayer:
         """x_pad_zero: the channels of x beyond spec.cin are known to hold zeros (true for tensors made by
         `to_device`); lets the first-layer kernel fetch whole image rows per request."""
         if y is None:
-            y = self.alloc_out(x)
+            with _on(stream, x.device):
+                y = self.alloc_out(x)
         name = "rt3d_conv3d_dense" if self.dense else "rt3d_conv3d_sparse"
         if not _unwrapped(name):
             fn = B.rt3d_conv3d_dense if self.dense else B.rt3d_conv3d_sparse
@@ -178,7 +179,8 @@ class LinearW4Layer:
                  x_pad_zero=False):
         """The arguments of a ConvLayer; there is one kernel family, and x's padding never matters."""
         if y is None:
-            y = self.alloc_out(x)
+            with _on(stream, x.device):
+                y = self.alloc_out(x)
         B.rt3d_linear_w4(x, self.weights, self.bias, y, self.spec.relu if relu is None else relu, stream)
         return y
 
@@ -187,14 +189,16 @@ def maxpool(x: torch.Tensor, c: int, pool, y: torch.Tensor | None = None, stream
     n, t, h, w, cs = x.shape
     ext = [(d + 2 * p - k) // s + 1 for d, p, k, s in zip((t, h, w), pool.pad, pool.k, pool.stride)]
     if y is None:
-        y = torch.zeros((n, ext[0], ext[1], ext[2], cs), dtype=x.dtype, device=x.device)
+        with _on(stream, x.device):
+            y = torch.zeros((n, ext[0], ext[1], ext[2], cs), dtype=x.dtype, device=x.device)
     B.rt3d_maxpool3d(B.tensor_desc(x, c), pool.k, pool.stride, pool.pad, B.tensor_desc(y, c), stream)
     return y
 
 
 def add_relu(a: torch.Tensor, b: torch.Tensor, c: int, relu=True, y: torch.Tensor | None = None, stream=None):
     if y is None:
-        y = torch.zeros_like(a)
+        with _on(stream, a.device):
+            y = torch.zeros_like(a)
     B.rt3d_add_relu(B.tensor_desc(a, c), B.tensor_desc(b, c), relu, B.tensor_desc(y, c), stream)
     return y
 
@@ -243,7 +247,8 @@ class _NotedForward:
 
     def forward(self, x: torch.Tensor, algo=B.ALGO_AUTO, keep=None, stream=None, **kw) -> torch.Tensor:
         if keep is not None or any(v is not None for v in kw.values()) or B.is_planning() or not _unwrapped(*_FUNCTIONS):
-            return self._forward(x, algo, keep, stream, **kw)
+            with _on(stream, x.device):
+                return self._forward(x, algo, keep, stream, **kw)
         noted = self.__dict__.setdefault("_noted", {})
         # torch.Size, dtype and device hash by value; the current device and whether a stream is named decide the streams
         key = (x.shape, x.stride(), x.dtype, x.device, algo, stream is None, B.concurrent(), torch.cuda.current_device())
@@ -259,7 +264,7 @@ class _NotedForward:
             del noted[key]
         seq = B.CallSequence(ptr, B.current_stream_ptr() if stream is None else int(stream))
         changes = _layer_changes
-        with seq.noting():
+        with seq.noting(), _on(stream, x.device):                       # buffers that the pass makes are zeroed on its stream
             out = self._forward(x, algo, None, stream)
         buffers = {b.data_ptr(): b for b in self.ws.bufs.values()}      # kept alive as long as the noted calls
         if ptr not in buffers:

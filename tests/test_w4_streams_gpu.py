@@ -1,4 +1,4 @@
-"""4-bit layers on a stream that is not the current one: what a call makes for itself is in that stream's order."""
+"""Layers on a stream that is not the current one: what a call makes for itself is in that stream's order."""
 import numpy as np
 import pytest
 import torch
@@ -55,3 +55,51 @@ def test_the_default_stream_by_its_handle():
     codes, scales = codes_of(w, group, False)
     np.testing.assert_array_equal(layer.weights.codes.cpu().numpy(), codes)
     np.testing.assert_array_equal(layer.weights.scales.float().cpu().numpy(), scales)
+
+
+@pytest.mark.parametrize("kind", ["4-bit", "dense"])
+def test_an_output_made_by_the_call_is_zeroed_before_the_kernel(kind):
+    """The current stream is busy: zeros that it brought would come after the products."""
+    m, k = 40, 64
+    w = weights(m, k, 3)
+    make = nets.LinearW4Layer if kind == "4-bit" else lambda sp, w, b, group: nets.ConvLayer(sp, w.reshape(m, k, 1, 1, 1), b, None, dense=True)
+    layer = make(spec(m, k), w, np.ones(m, np.float32), 32)
+    x = torch.rand(3, 1, 1, 1, k, device="cuda").to(torch.bfloat16)
+    want = layer(x).clone()
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    torch.cuda._sleep(BUSY)
+    y = layer(x, stream=side.cuda_stream)
+    torch.cuda.synchronize()
+    assert bool((want != 0).any()) and torch.equal(y, want)
+
+
+def test_pools_and_sums_that_make_their_output():
+    pool = synth.PoolSpec("p", (2, 2, 2), (2, 2, 2), (0, 0, 0))
+    a, b = (torch.rand(2, 4, 6, 6, 16, device="cuda").to(torch.bfloat16) for _ in range(2))
+    for call in (lambda s: nets.maxpool(a, 16, pool, stream=s), lambda s: nets.add_relu(a, b, 16, stream=s)):
+        want = call(None).clone()
+        torch.cuda.synchronize()
+        side = torch.cuda.Stream()
+        torch.cuda._sleep(BUSY)
+        y = call(side.cuda_stream)
+        torch.cuda.synchronize()
+        assert bool((want != 0).any()) and torch.equal(y, want)
+
+
+@pytest.mark.parametrize("keep", [False, True])
+def test_a_networks_first_pass_on_a_side_stream(keep):
+    plan = [synth.ConvSpec("conv1", 3, 16, (3, 3, 3), (1, 1, 1), (1, 1, 1), True), synth.PoolSpec("pool1", (2, 2, 2), (2, 2, 2), (0, 0, 0))]
+    L = synth.make_layer(plan[0], 7, 0, 4, 4, "bernoulli", 0.5)
+    layers = {"conv1": nets.ConvLayer(plan[0], L["w"], L["bias"], L["mask"], 4, 4, torch.bfloat16)}
+    fc = [nets.LinearW4Layer(spec(200, 512, True), weights(200, 512, 1), np.ones(200, np.float32), 32)]
+    x = nets.to_device(synth.make_input(7, (2, 4, 8, 8, 3)))
+    first = {}
+    want = nets.C3DNet(plan, layers, fc_layers=fc).forward(x, keep=first).clone()
+    net = nets.C3DNet(plan, layers, fc_layers=fc)                    # without buffers
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    torch.cuda._sleep(BUSY)
+    y = net.forward(x, keep={} if keep else None, stream=side.cuda_stream)
+    torch.cuda.synchronize()
+    assert bool((want != 0).any()) and torch.equal(y, want)

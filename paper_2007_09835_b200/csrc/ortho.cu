@@ -169,14 +169,29 @@ __device__ __forceinline__ void split_half(float v, __half& hi, __half& lo) {
   lo = __float2half_rn(v - __half2float(hi));
 }
 
+// The steps as the device needs them: how many each run takes, and their coefficients.
+struct RunSteps {
+  int runs;
+  uint8_t steps[kRuns];
+  float abc[kMostSteps][3];
+};
+
 // The matrix of run r is F_r times what is held.  F_0 is the source over its norm and eps, of which a power of two is taken here,
-// which rounds nothing but what falls under fp16; where eps leaves less than 1/32 of a norm of one (a run enlarges by at most 50),
-// the next run's matrix is held times a power of two as well, so that the smallest gradients keep their bits too.
+// which rounds nothing but what falls under fp16.  `size` bounds the matrix's singular values through the steps (|p| of a step is at most
+// |a| + |b| s^2 + |c| s^4 there, and no step leaves more than 1.9): where a run leaves less than one, because eps is more than the norm or
+// because its steps shrink, the next run's matrix is held times the power of two that brings that bound next to one, so that no
+// gradient and no step takes the bits of the values under fp16's.
 // factors[r]: F_r^2, for G; factors[kRuns + r]: F_r / F_(r + 1), for X.
-__device__ void write_factors(double f, int runs, float* __restrict__ factors) {
-  for (int r = 0; r < runs; ++r) {
+__device__ void write_factors(double f, double size, const RunSteps& steps, float* __restrict__ factors) {
+  int step = 0;
+  for (int r = 0; r < steps.runs; ++r) {
+    for (int i = 0; i < steps.steps[r]; ++i, ++step) {
+      const double square = size * size;
+      size *= fabs(steps.abc[step][0]) + square * (fabs(steps.abc[step][1]) + square * fabs(steps.abc[step][2]));
+      if (size > 1.9) size = 1.9;
+    }
     double next = 1.0;
-    if (r + 1 < runs && f < 1.0 / 32) next = exp2(ceil(log2(f * 64.0)));
+    if (r + 1 < steps.runs && size > 0.0 && size < 1.0) next = scalbn(1.0, ilogb(size) + 1);
     factors[r] = float(f * f);
     factors[kRuns + r] = float(f / next);
     f = next;
@@ -187,7 +202,8 @@ __device__ void write_factors(double f, int runs, float* __restrict__ factors) {
 template <typename T, bool kVec>
 __global__ void __launch_bounds__(256)
 split_kernel(Source<T> s, int m, int k, const double* __restrict__ sums, double eps, int turned, __half* __restrict__ hi,
-             __half* __restrict__ lo, long long x_pitch, int runs, float* __restrict__ factors, unsigned* __restrict__ arrived) {
+             __half* __restrict__ lo, long long x_pitch, const __grid_constant__ RunSteps steps, float* __restrict__ factors,
+             unsigned* __restrict__ arrived) {
   pdl_entry();
   __shared__ double part[8];
   __shared__ float tile[32][133];
@@ -215,7 +231,8 @@ split_kernel(Source<T> s, int m, int k, const double* __restrict__ sums, double 
     const double power = scalbn(1.0, e);
     scale_s[0] = scalbnf(1.f, first); scale_s[1] = scalbnf(1.f, up - first);
     if (blockIdx.x == 0)
-      write_factors(number ? 1.0 / ((norm + eps) * power) : norm == 0.0 ? 1.0 : __longlong_as_double(0x7fffffffffffffffll), runs, factors);
+      write_factors(number ? 1.0 / ((norm + eps) * power) : norm == 0.0 ? 1.0 : __longlong_as_double(0x7fffffffffffffffll),
+                    number ? norm / (norm + eps) : 0.0, steps, factors);
   }
   __syncthreads();
   const float scale0 = scale_s[0], scale1 = scale_s[1];
@@ -1110,8 +1127,12 @@ rt3d_status direction(const Source<T>& src, int m, int k, const Plan& plan, int 
   const Matrix* x = &ws.all[kX0];
   int parts = !exact && sizeof(T) == 2 ? 1 : 2;
   __half* lo = parts == 2 ? x->lo : nullptr;
-  int runs = 0;
-  for (int done = 0; done < plan.steps; ++runs) done += run_steps(plan, done, short_x ? 1 : runs ? 3 : first);
+  RunSteps runs{};
+  for (int done = 0; done < plan.steps; ++runs.runs) {
+    runs.steps[runs.runs] = uint8_t(run_steps(plan, done, short_x ? 1 : runs.runs ? 3 : first));
+    done += runs.steps[runs.runs];
+  }
+  std::memcpy(runs.abc, plan.abc, sizeof(runs.abc));
   const long long blocks = ceil_div64(m, 32) * ceil_div64(k, 128);
   if (blocks >= (1ll << 31)) return RT3D_ERR_UNSUPPORTED;
   LaunchSetup l2(dim3(unsigned(blocks)), dim3(256), 0, st);

@@ -293,7 +293,13 @@ struct Stage {
   // columns of an accumulator: with both parts of B side by side, hi hi and hi lo are one product where kCols is 64 (120 clocks for 16 of
   // the sum of all three parts, 168 one after another)
   static constexpr int kAcc = 128;
+  static constexpr int kSumsAt = 2 * kAcc, kTmemCols = 512;            // behind the accumulators: kCols of sums so far (a power of two in all)
 };
+// The tensor core cuts addends off as it adds, which in sums of one sign (the diagonal of X X^T) goes one way: an accumulator takes 512 of a
+// sum, then the other one goes on while its values are added, rounded to nearest, to those before it, which lie in tensor memory too.
+// An update's direction against 64 bits, of |O|, with one accumulator to a sum and with this: 4096 x 8192 2.0e-4 and 3.4e-5, 1500 x 1500
+// 9.5e-5 and 4.4e-5, 130 x 2^18 2.2e-4 and 5.9e-6 (of noise), for 2 to 5 % of the time; segments of 256 halve the larger ones again for 2 % more.
+constexpr int kSegment = 8;                          // chunks of 64, at most
 
 enum { kOutParts = 0, kOutDirection = 1, kOutUpdate = 2 };
 
@@ -319,6 +325,7 @@ struct Problem {
   int b_rows;                                        // B's own rows
   int symmetric;                                     // so is C: tiles on and under the diagonal
   int chunks;
+  int segment, segments;                             // chunks of an accumulator, accumulators of a sum (of the largest share of one)
   int tiles_m, n_tiles;
   int rows, cols;                                    // what of C exists (symmetric: all of the tiles)
 };
@@ -502,11 +509,50 @@ __device__ __forceinline__ void sts128(uint32_t addr, const uint4& v) {
   asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
 }
 
+__device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&r)[32]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
+      "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};"
+      ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]),
+        "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]),
+        "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]));
+  asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void add_sums(uint32_t sums, uint32_t (&r)[32]) {
+  uint32_t so_far[32];
+  tmem_ld32(sums, so_far);
+#pragma unroll
+  for (int e = 0; e < 32; ++e) r[e] = __float_as_uint(__uint_as_float(so_far[e]) + __uint_as_float(r[e]));
+}
+// A thread has the columns half * 32 .. + 31 of every 64 of its row.  Adds the accumulators of `segments` segments to its sums; `n` counts
+// the accumulators.
+template <int kCols>
+__device__ __forceinline__ bool drain(const Problem& p, uint32_t lanes, int half, int segments, uint32_t& n, int lane, Barriers* bars, int32_t* err) {
+  typedef Stage<kCols> S;
+  for (int g = 0; g < segments; ++g, ++n) {
+    const uint32_t buf = n & 1u;
+    if (!mbar_wait_warp(smem_u32(&bars->tmem_full[buf]), (n >> 1) & 1u, bars, err, 4)) return false;
+    tc_fence_after();
+#pragma unroll 1
+    for (int c = half * 32; c < kCols; c += 64) {
+      uint32_t r[32];
+      __syncwarp();
+      tmem_ld_acc(lanes + buf * S::kAcc + c, true, kCols == 64 && p.parts == 3 ? uint32_t(kCols) : 0u, r);
+      if (g) add_sums(lanes + S::kSumsAt + c, r);
+      tmem_st32(lanes + S::kSumsAt + c, r);
+    }
+    tc_fence_before();
+    __syncwarp();
+    if (lane == 0) mbar_arrive(smem_u32(&bars->tmem_empty[buf]));
+  }
+  return true;
+}
+
 // The parts of a tile of 128 x 64 through shared memory and out in whole rows; D comes the same way, to the places its thread then
 // writes.  (16-byte accesses of a row each, which touch 32 lines, kept the SM's load and store unit busy for 2000 clocks of a
 // step's 8000.)  Called by all 256 threads.
 template <int kCols>
-__device__ __forceinline__ void finish_staged(const Problem& p, const Maps* maps, const TileAt& t, uint32_t taddr, int row, int half, float alpha, uint32_t base,
+__device__ __forceinline__ void finish_staged(const Problem& p, const Maps* maps, const TileAt& t, uint32_t taddr, uint32_t sums, int row, int half, float alpha, uint32_t base,
                                               uint32_t tmem_full, uint32_t full_parity, uint32_t d_parity, Barriers* bars, int32_t* err) {
   typedef Stage<kCols> S;
   const bool leader = threadIdx.x == 64, add = p.d_hi != nullptr;
@@ -528,6 +574,7 @@ __device__ __forceinline__ void finish_staged(const Problem& p, const Maps* maps
     uint32_t r[32];
     __syncwarp();
     tmem_ld_acc(taddr + half * 32, true, p.parts == 3 ? uint32_t(kCols) : 0u, r);
+    if (sums) add_sums(sums + half * 32, r);
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
       const uint32_t at = line + (((half * 4 + u) ^ (row & 7)) << 4);
@@ -621,7 +668,7 @@ product_kernel(const __grid_constant__ ProductArgs<kProblems> a) {
     for (int q = int(threadIdx.x) - 64; q < (kProblems > 1 ? kMatrices * 4 : 0); q += kProductThreads - 64) tma_prefetch_map(&a.m[0].rows128[0] + q);
   if (warp == 1) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;"
-                 ::"r"(smem_u32(&bars->tmem_base)), "r"(uint32_t(2 * S::kAcc)) : "memory");
+                 ::"r"(smem_u32(&bars->tmem_base)), "r"(uint32_t(S::kTmemCols)) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
   tc_fence_before();
@@ -633,6 +680,7 @@ product_kernel(const __grid_constant__ ProductArgs<kProblems> a) {
 
   int stage = 0;                                     // of this role: the ring and the accumulators go on from step to step
   uint32_t phase = 0, n = 0, adds = 0;
+  bool joined = false;
 #pragma unroll 1
   for (int s = 0; s < a.n_steps; ++s) {
     int n_items = 0;
@@ -692,11 +740,20 @@ product_kernel(const __grid_constant__ ProductArgs<kProblems> a) {
         const TileAt t = item == cta ? t0 : tile_at<kCols>(steps, s, item);
         const Problem& p = steps.p[t.problem];
         const bool one = kCols == kTile && p.same && t.i == t.j;
-        const uint32_t buf = n & 1u, d = tmem + buf * S::kAcc;
-        if (!mbar_wait_warp(smem_u32(&bars->tmem_empty[buf]), ((n >> 1) & 1u) ^ 1u, bars, a.err, 2)) break;
-        tc_fence_after();
+        uint32_t buf = 0, d = 0;
         const int c_first = p.chunks * split / a.splits, c_last = p.chunks * (split + 1) / a.splits;
-        for (int c = c_first; c < c_last; ++c) {
+        for (int c = c_first, left = 0; c < c_last; ++c, --left) {
+          const bool first = left == 0;              // of an accumulator
+          if (first) {
+            left = p.segment;
+            if (c > c_first) {
+              if (elected) umma_commit(smem_u32(&bars->tmem_full[buf]));
+              ++n;
+            }
+            buf = n & 1u; d = tmem + buf * S::kAcc;
+            if (!mbar_wait_warp(smem_u32(&bars->tmem_empty[buf]), ((n >> 1) & 1u) ^ 1u, bars, a.err, 2)) { ok = false; break; }
+            tc_fence_after();
+          }
           if (!mbar_wait_warp(smem_u32(&bars->full[stage]), phase, bars, a.err, 3)) { ok = false; break; }
           tc_fence_after();
           const uint32_t at = base + stage * a.stage_bytes, b_at = one ? at : at + a.b_at, b_lo_at = one ? at + kRowsBytes : b_at + S::kColsBytes;
@@ -709,7 +766,7 @@ product_kernel(const __grid_constant__ ProductArgs<kProblems> a) {
           const uint64_t b_lo = b_turned ? smem_desc_rows(b_lo_at) : smem_desc_sw128(b_lo_at);
           if (elected) {
             const bool both = kCols == 64 && p.parts == 3;
-            const uint32_t more = c > c_first ? 1u : 0u;
+            const uint32_t more = first ? 0u : 1u;
             if (both) {                              // hi hi and hi lo side by side
               const uint32_t wide = instr_desc_f16<128>(a_turned, b_turned);
 #pragma unroll
@@ -739,24 +796,30 @@ product_kernel(const __grid_constant__ ProductArgs<kProblems> a) {
         const TileAt t = item == cta ? t0 : tile_at<kCols>(steps, s, item);
         const Problem& p = steps.p[t.problem];
         const float alpha = p.factor ? p.alpha * __ldcg(p.factor) : p.alpha;
-        const uint32_t buf = n & 1u, at = tmem + (uint32_t(quad * 32) << 16) + buf * S::kAcc;
+        const uint32_t lanes = tmem + (uint32_t(quad * 32) << 16);
+        int segments = p.segments;
+        if (a.splits > 1) segments = (p.chunks * (split + 1) / a.splits - p.chunks * split / a.splits + p.segment - 1) / p.segment;
+        const bool drained = drain<kCols>(p, lanes, half, segments - 1, n, lane, bars, a.err);
+        const uint32_t buf = n & 1u, at = lanes + buf * S::kAcc, sums = segments > 1 ? lanes + S::kSumsAt : 0u;
         Addend d;
         const long long d_at = (t.i * kTile + row) * p.pitch + t.j * kCols;
         if (kCols == 64 && p.out == kOutParts) {
-          finish_staged<kCols>(p, a.m, t, at, row, half, alpha, base, smem_u32(&bars->tmem_full[buf]), (n >> 1) & 1u, adds & 1u, bars, a.err);
+          finish_staged<kCols>(p, a.m, t, at, sums, row, half, alpha, base, smem_u32(&bars->tmem_full[buf]), (n >> 1) & 1u, adds & 1u, bars, a.err);
           adds += p.d_hi != nullptr;
           tc_fence_before();
           __syncwarp();
           if (lane == 0) mbar_arrive(smem_u32(&bars->tmem_empty[buf]));
           continue;
         }
-        if (!mbar_wait_warp(smem_u32(&bars->tmem_full[buf]), (n >> 1) & 1u, bars, a.err, 4)) break;
+        if (!drained || !mbar_wait_warp(smem_u32(&bars->tmem_full[buf]), (n >> 1) & 1u, bars, a.err, 4)) break;
         tc_fence_after();
         if (a.splits > 1) {          // this CTA's only tile: its part goes where the stages were, which every product has read
-          store_partial_row(at, kCols, true, reinterpret_cast<float*>(smem_raw + (base - smem_u32(smem_raw))) + row * kPartRow, half * 32, 64);
+          store_partial_row(at, kCols, true, reinterpret_cast<float*>(smem_raw + (base - smem_u32(smem_raw))) + row * kPartRow, half * 32, 64,
+                            sums ? sums - at : 0u);
         } else {
 #pragma unroll 1
-          for (int c0 = half * 16; c0 < kCols; c0 += 32) {
+          for (int u = 0; u < kCols / 32; ++u) {
+            const int c0 = (u >> 1) * 64 + half * 32 + (u & 1) * 16;
             uint32_t r[16];
             if (p.d_hi) d.load(p, d_at + c0);
             __syncwarp();
@@ -769,6 +832,11 @@ product_kernel(const __grid_constant__ ProductArgs<kProblems> a) {
 #pragma unroll
               for (int e = 0; e < 16; ++e) v[e] += __uint_as_float(r[e]);
             }
+            if (sums) {
+              tmem_ld16(sums + c0, r);
+#pragma unroll
+              for (int e = 0; e < 16; ++e) v[e] += __uint_as_float(r[e]);
+            }
             finish16<kCols>(a, p, t, row, c0, v, alpha, d);
           }
         }
@@ -777,6 +845,7 @@ product_kernel(const __grid_constant__ ProductArgs<kProblems> a) {
         if (lane == 0) mbar_arrive(smem_u32(&bars->tmem_empty[buf]));
         if (a.splits > 1) {
           cluster_sync_all();
+          joined = true;
           if (!bars->abort_flag) {
             constexpr int units = kCols / 16;
             const int u1 = units * (split + 1) / a.splits;
@@ -807,7 +876,7 @@ product_kernel(const __grid_constant__ ProductArgs<kProblems> a) {
   if (a.splits > 1) {
     // the results' warps have waited once, the others not; and nobody leaves while its part is still being read
     __syncwarp();
-    if (warp < 2 || n == 0) cluster_sync_all();
+    if (warp < 2 || !joined) cluster_sync_all();
     cluster_sync_all();
   }
   if (bars->abort_flag) {
@@ -819,7 +888,7 @@ product_kernel(const __grid_constant__ ProductArgs<kProblems> a) {
   __syncthreads();
   if (warp == 1) {
     tc_fence_after();
-    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(uint32_t(2 * S::kAcc)) : "memory");
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(uint32_t(S::kTmemCols)) : "memory");
   }
 }
 
@@ -1022,6 +1091,12 @@ struct Runner {
     for (int i = 0; i < a.steps.first[a.n_steps]; ++i) {
       if (a.steps.p[i].parts >= 2) a_parts = 2;
       if (a.steps.p[i].parts == 3) b_parts = 2;
+    }
+    for (int i = 0; i < a.steps.first[a.n_steps]; ++i) {           // segments as long as one another: one is added while the next one's products run
+      Problem& p = a.steps.p[i];
+      const int share = ceil_div(p.chunks, a.splits);
+      p.segments = ceil_div(share, kSegment);
+      p.segment = ceil_div(share, p.segments);
     }
     a.b_at = a_parts * kRowsBytes;
     a.stage_bytes = a.b_at + b_parts * Stage<kCols>::kColsBytes;

@@ -8,8 +8,8 @@
 // at most three steps to a run (which enlarge by at most 41 = 3.4445^3) nothing of weight is lost: against 64 bits 4e-7 to 5e-6 of |O| for
 // matrices whose singular values fall off as 1 to 1/i^2, where five steps in one run give NaN.
 // Values enter the tensor cores as fp16 parts, v = hi + lo (22 bits), products as hi hi + hi lo + lo hi with fp32 sums.  fp16's 11 bits
-// against bf16's 8: a bf16 gradient is its own hi part, and the X before the last steps of rt3d_orthogonalize, whose result is bf16,
-// needs no lo part.  Matrices are held times a power of two (2^14, 2^10 for P and Q) so that lo parts stay normal numbers.
+// against bf16's 8, and a bf16 gradient is its own hi part.  (The X before the last steps without its lo part, for a result in bf16, leaves
+// 1.0e-3 of |O| beside that result's own rounding, 1.7e-3, in roundings that go the other way; it saved 3 to 16 %.)  Matrices are held times a power of two (2^14, 2^10 for P and Q) so that lo parts stay normal numbers.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
@@ -316,7 +316,7 @@ struct Problem {
   float alpha, beta, diag;
   const float* factor;                               // nullptr: 1
   const __half *d_hi, *d_lo;                         // D, or nullptr
-  __half *c_hi, *c_lo;                               // kOutParts; c_lo may be nullptr
+  __half *c_hi, *c_lo;                               // kOutParts
   long long pitch;                                   // of C and D
   int parts;                                         // 1: hi hi; 2: hi hi + lo hi; 3: and hi lo
   int same;                                          // A and B are the same matrix: a tile on the diagonal loads it once
@@ -435,7 +435,7 @@ __device__ __forceinline__ void finish16(const ProductArgs<kProblems>& a, const 
     for (int q = 0; q < 2; ++q)
       if (j + 8 * q < p.cols) {                      // the pitch is a multiple of 8: what lies behind the last column is padding
         *reinterpret_cast<uint4*>(p.c_hi + at + 8 * q) = reinterpret_cast<const uint4*>(h)[q];
-        if (p.c_lo) *reinterpret_cast<uint4*>(p.c_lo + at + 8 * q) = reinterpret_cast<const uint4*>(l)[q];
+        *reinterpret_cast<uint4*>(p.c_lo + at + 8 * q) = reinterpret_cast<const uint4*>(l)[q];
       }
     return;
   }
@@ -604,8 +604,7 @@ __device__ __forceinline__ void finish_staged(const Problem& p, const Maps* maps
   asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   epilogue_bar_sync(256);
   if (leader && ok) {
-    const int parts = p.c_lo ? 2 : 1;
-    for (int q = 0; q < parts; ++q) tma_store_2d(&maps[p.c].rows128[q], out + q * kRowsBytes, t.j * kCols, t.i * kTile);
+    for (int q = 0; q < 2; ++q) tma_store_2d(&maps[p.c].rows128[q], out + q * kRowsBytes, t.j * kCols, t.i * kTile);
     asm volatile("cp.async.bulk.commit_group;" ::: "memory");
   }
 }
@@ -1047,9 +1046,9 @@ struct Runner {
     p->rows = x.rows; p->cols = x.cols;
     p->factor = factor; p->alpha = 1.f / kPScale;
   }
-  void out_parts(Problem* p, int c, int parts = 2) const {
+  void out_parts(Problem* p, int c) const {
     const Matrix& m = matrix(c);
-    p->out = kOutParts; p->c = c; p->c_hi = m.hi; p->c_lo = parts == 2 ? m.lo : nullptr; p->pitch = m.pitch;
+    p->out = kOutParts; p->c = c; p->c_hi = m.hi; p->c_lo = m.lo; p->pitch = m.pitch;
     p->rows = m.rows; p->cols = m.cols;
   }
 
@@ -1174,18 +1173,8 @@ int run_steps(const Plan& plan, int done, int most) {
   return steps;
 }
 
-// Parts of the X that the step `done` reads, for a result in bf16: what its rounding leaves in directions of small singular values is
-// enlarged by the steps left.  2^-12 of fp16 times 12 is 2^-8.4 where such directions are all of X, and they never are: with singular
-// values as 1 / i^2, 2.0e-3 of |O| in all, of which bf16's rounding is 1.7e-3 (enlarged by 41: 3.6e-3).
-int later_parts(const Plan& plan, int done) {
-  double left = 1.0;
-  for (int i = done; i < plan.steps; ++i) left *= plan.most[i] > 1.0 ? plan.most[i] : 1.0;
-  return left <= 12.0 ? 1 : 2;
-}
-
-// `first`: most steps of the first run; `exact`: two parts of every X; else one of the first where one holds it.
 template <typename T>
-rt3d_status direction(const Source<T>& src, int m, int k, const Plan& plan, int first, bool exact, const Workspace& ws, const Result& res,
+rt3d_status direction(const Source<T>& src, int m, int k, const Plan& plan, const Workspace& ws, const Result& res,
                       const DeviceInfo& dev, cudaStream_t st) {
   Runner r{dev, st, ws};
   if (!r.make_maps()) return RT3D_ERR_CUDA;
@@ -1200,11 +1189,11 @@ rt3d_status direction(const Source<T>& src, int m, int k, const Plan& plan, int 
                                                  : cudaLaunchKernelEx(&l1.cfg, square_sums_kernel<T, false, false>, src, m, k, ws.sums));
   if (s != RT3D_OK) return s;
   const Matrix* x = &ws.all[kX0];
-  int parts = !exact && sizeof(T) == 2 ? 1 : 2;
+  int parts = sizeof(T) == 2 && !src.momentum ? 1 : 2;           // a bf16 gradient is its own hi part
   __half* lo = parts == 2 ? x->lo : nullptr;
   RunSteps runs{};
   for (int done = 0; done < plan.steps; ++runs.runs) {
-    runs.steps[runs.runs] = uint8_t(run_steps(plan, done, short_x ? 1 : runs.runs ? 3 : first));
+    runs.steps[runs.runs] = uint8_t(run_steps(plan, done, short_x ? 1 : runs.runs ? 3 : 2));
     done += runs.steps[runs.runs];
   }
   std::memcpy(runs.abc, plan.abc, sizeof(runs.abc));
@@ -1227,7 +1216,7 @@ rt3d_status direction(const Source<T>& src, int m, int k, const Plan& plan, int 
   };
   int cur = kX0, other = kX1;
   for (int done = 0, run = 0; done < plan.steps; ++run) {
-    const int steps = run_steps(plan, done, short_x ? 1 : run ? 3 : first);
+    const int steps = run_steps(plan, done, short_x ? 1 : run ? 3 : 2);
     int g = kG0, g2 = kG1, p = kP0, p2 = kP1, q = -1, q_next = kQ0;
     const int cols = n_fused ? 64 : kTile;
     if (short_x) {
@@ -1280,8 +1269,8 @@ rt3d_status direction(const Source<T>& src, int m, int k, const Plan& plan, int 
     if (last) {
       c->out = res.out; c->alpha /= kXScale;
     } else {
-      parts = exact ? 2 : later_parts(plan, done);
-      r.out_parts(c, other, parts);
+      parts = 2;
+      r.out_parts(c, other);
     }
     auto results = [&](auto& args) {
       args.turned = res.turned; args.bf = res.bf; args.w = res.w; args.mask = res.mask;
@@ -1315,7 +1304,7 @@ rt3d_status orthogonalize(const T* g, int64_t pitch, int m, int k, const Plan& p
   Workspace ws;
   workspace_of(m, k, base, &ws);
   const Result res{kOutDirection, m > k, out, nullptr, nullptr, 0.f, 0.f, (long long)out_pitch};
-  return direction(Source<T>{g, pitch, nullptr, nullptr, 0.f, 0}, m, k, plan, 3, false, ws, res, dev, st);
+  return direction(Source<T>{g, pitch, nullptr, nullptr, 0.f, 0}, m, k, plan, ws, res, dev, st);
 }
 
 template <typename T>
@@ -1324,7 +1313,7 @@ rt3d_status update(float* w, float* momentum, const T* g, const uint8_t* mask, i
   Workspace ws;
   workspace_of(m, k, base, &ws);
   const Result res{kOutUpdate, m > k, nullptr, w, mask, float(1.0 - double(p.lr) * p.weight_decay), float(double(p.lr) * p.scale), k};
-  return direction(Source<T>{g, k, momentum, mask, p.mu, p.nesterov}, m, k, plan, 2, true, ws, res, dev, st);
+  return direction(Source<T>{g, k, momentum, mask, p.mu, p.nesterov}, m, k, plan, ws, res, dev, st);
 }
 
 }  // namespace

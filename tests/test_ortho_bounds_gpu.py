@@ -100,3 +100,12 @@ def test_long_sums(m, k):
     check(noise(m, k, m) * 1e-3)
     if m * k <= 1 << 25:
         check(noise(m, k, m).abs() * 1e-3)           # of one sign
+
+
+# ----------------------------------------------------------------------------------------------- bf16 results are the fp32 ones, rounded
+@pytest.mark.parametrize("m,k", [(64, 576), (129, 127), (300, 517), (512, 4096), (1300, 1100), (130, 20000)])
+def test_directions_are_rounded_once(m, k):
+    u = (orthoref.matrix("falling", m, k, 3) * 1e-3).float().cuda()
+    out = torch.empty(m, k, dtype=torch.bfloat16, device="cuda")
+    rt3d.rt3d_orthogonalize(u, out, workspace(m, k))
+    assert torch.equal(out, fp32_direction(u).to(torch.bfloat16))

@@ -102,6 +102,20 @@ def test_long_sums(m, k):
         check(noise(m, k, m).abs() * 1e-3)           # of one sign
 
 
+# ------------------------------------------------------------------------------------ few directions, numbers of steps, coefficients
+@pytest.mark.parametrize("steps", [1, 2, 3, 5, 7, 10, 16])
+@pytest.mark.parametrize("rank,m,k", [(1, 60, 400), (16, 256, 1500), (3, 1300, 200), (40, 300, 5000), (5, 1100, 1200), (2, 2000, 3000)])
+def test_few_directions(rank, m, k, steps):
+    check(of_rank(rank, m, k), steps, few=True)
+
+
+@pytest.mark.parametrize("coefs", [[(1.5, -0.5, 0.0)] * 8, [(2.0, -1.5, 0.5)] * 6, [(1.875, -1.25, 0.375)] * 3, [(-1.0, 0.0, 0.0)], [(1.0, 0.0, 0.0)] * 16,
+                                   [(7.5, -21.0, 14.5), (2.0, -1.0, 0.17), (2.2, -1.6, 0.4), (1.875, -1.25, 0.375), (1.875, -1.25, 0.375)], [(1.0, -1.0, 0.0)] * 2])
+@pytest.mark.parametrize("rank,m,k", [(1, 60, 400), (16, 256, 1500), (60, 80, 60)])
+def test_other_coefficients(coefs, rank, m, k):
+    check(of_rank(rank, m, k), len(coefs), coefs)
+
+
 # ----------------------------------------------------------------------------------------------- bf16 results are the fp32 ones, rounded
 @pytest.mark.parametrize("m,k", [(64, 576), (129, 127), (300, 517), (512, 4096), (1300, 1100), (130, 20000)])
 def test_directions_are_rounded_once(m, k):

@@ -687,8 +687,9 @@ product_kernel(const __grid_constant__ ProductArgs<kProblems> a) {
     TileAt t0{0, 0, 0};                              // this CTA's first, found while the others end the last step
     if (cta < n_items) t0 = tile_at<kCols>(steps, s, cta);
     if (kProblems > 1 && s > 0) {
-      // What the last step has written is what this one's copies read: both through the same proxy, so that once the stores are
-      // complete (which this waits for) the barrier orders the two.
+      // What the last step's bulk stores have written is what this one's copies read, in other CTAs.  The stores' completion makes the
+      // values visible to the thread that waits for it, the barrier passes that on, and the fence puts the copies, which go through the
+      // other proxy, behind it.
       if (threadIdx.x == 64) tma_store_wait_all();
       if (a.one_cluster) {                           // a release and an acquire of the cluster
         __syncwarp();
@@ -697,6 +698,7 @@ product_kernel(const __grid_constant__ ProductArgs<kProblems> a) {
         grid_barrier(a.arrived, unsigned(s) * gridDim.x, bars, a.err);
         if (bars->abort_flag) break;                 // this CTA's steps end here; the others' waits run out
       }
+      asm volatile("fence.proxy.async.global;" ::: "memory");
     }
     if (warp == 0) {
       // ---------------------------------------------------------------- loads

@@ -594,6 +594,16 @@ def _dtype_code(t) -> int:
         raise ValueError(f"expected float32 or bfloat16, got {t.dtype}") from None
 
 
+def _on_device(index: int, *tensors):
+    """Refuses tensors (None: none) that are not on CUDA device `index` (-1: the host), and a device that is not the current one, on
+    which calls are launched: a kernel would read host memory, or another device's."""
+    if index < 0 or any(t is not None and t.get_device() != index for t in tensors):
+        raise ValueError("the tensors of a call have to be on one CUDA device")
+    import torch
+    if index != torch.cuda.current_device():
+        raise ValueError(f"the tensors are on CUDA device {index}, the current one is {torch.cuda.current_device()}")
+
+
 def _matrix(t, m: int, k: int):
     """(address, dtype, pitch) of a device tensor [m][k] (or [m][...] with k values each) whose rows are contiguous."""
     if t.dim() < 2 or t.shape[0] != m or t[0].numel() != k or not t[0].is_contiguous():
@@ -612,7 +622,8 @@ def rt3d_w4_scale_count(m: int, k: int, group: int) -> int:
 
 class W4Weights:
     """4-bit weights of m filters with k inputs on the device: codes (uint8), scales (bfloat16) and zero points (uint8, or
-    None), in the layout of include/rt3d.h.  Allocated here where they are not given; `zeros`: the tensor, or True to allocate it."""
+    None), in the layout of include/rt3d.h.  Allocated here where they are not given; `zeros`: the tensor, or True to allocate it.  Calls
+    take them where `index`, their CUDA device, is the current one."""
 
     def __init__(self, m: int, k: int, group: int = 128, codes=None, scales=None, zeros=None, device="cuda"):
         import torch
@@ -629,6 +640,7 @@ class W4Weights:
                                       ("zeros", self.zeros, torch.uint8, n_scales)):
             if t is not None and (t.dtype != dtype or t.numel() != count or not t.is_contiguous() or t.device != device):
                 raise ValueError(f"{name}: {count} contiguous values of {dtype} on {device} wanted")
+        self.index = self.codes.get_device()
         self.desc = W4(self.m, self.k, self.group, self.codes.data_ptr(), self.scales.data_ptr(),
                        None if self.zeros is None else self.zeros.data_ptr())
 
@@ -640,12 +652,12 @@ class W4Weights:
 
 def rt3d_w4_quantize(w, q: W4Weights, stream=None):
     """w: device tensor [m][k] or [m][N][Kt][Kh][Kw], float32 or bfloat16, rows contiguous (any row pitch); fills q."""
-    _check((_pycall_module or pycall()).w4_quantize(ADDRESS["rt3d_w4_quantize"], q.desc, w, stream), "rt3d_w4_quantize")
+    _check((_pycall_module or pycall()).w4_quantize(ADDRESS["rt3d_w4_quantize"], q.desc, q.index, w, stream), "rt3d_w4_quantize")
 
 
 def rt3d_w4_unpack(q: W4Weights, w, stream=None):
     """w: device tensor as for rt3d_w4_quantize (output): the values that the codes stand for."""
-    _check((_pycall_module or pycall()).w4_unpack(ADDRESS["rt3d_w4_unpack"], q.desc, w, stream), "rt3d_w4_unpack")
+    _check((_pycall_module or pycall()).w4_unpack(ADDRESS["rt3d_w4_unpack"], q.desc, q.index, w, stream), "rt3d_w4_unpack")
 
 
 def rt3d_linear_w4(x, q: W4Weights, bias, y, relu=False, stream=None):
@@ -653,10 +665,11 @@ def rt3d_linear_w4(x, q: W4Weights, bias, y, relu=False, stream=None):
     device tensor [m] or None."""
     seq = noting()
     if seq is None and not isinstance(x, Tensor) and not isinstance(y, Tensor):
-        status = (_pycall_module or pycall()).linear_w4(ADDRESS["rt3d_linear_w4"], x, q.desc, bias, y, relu, stream)
+        status = (_pycall_module or pycall()).linear_w4(ADDRESS["rt3d_linear_w4"], x, q.desc, q.index, bias, y, relu, stream)
         if status != OK:
             raise Rt3dError(status, "rt3d_linear_w4")
         return
+    _on_device(q.index, bias, *(t for t in (x, y) if not isinstance(t, Tensor)))
     xd = x if isinstance(x, Tensor) else tensor_desc(x, q.k)
     yd = y if isinstance(y, Tensor) else tensor_desc(y, q.m)
     _check(_lib.rt3d_linear_w4(ctypes.byref(xd), ctypes.byref(q.desc), _bias_ptr(bias), int(bool(relu)), ctypes.byref(yd),
@@ -692,6 +705,7 @@ def rt3d_orthogonalize(g, out, workspace, steps: int = 5, eps: float = 1e-7, coe
     row pitch); workspace: device tensor of at least rt3d_ortho_workspace(m, k) bytes; coefs: (a, b, c) of each step or None."""
     import torch
     m, k = g.shape[0], g[0].numel()
+    _on_device(g.get_device(), out, workspace)
     src, dtype, g_pitch = _matrix(g, m, k)
     dst, _, out_pitch = _matrix(out, m, k)
     if out.dtype != torch.bfloat16:
@@ -707,6 +721,7 @@ def rt3d_ortho_update(w, momentum, g, mask, workspace, lr: float, momentum_facto
     None), contiguous device tensors of equal extents."""
     import torch
     m, k = w.shape[0], w[0].numel()
+    _on_device(w.get_device(), momentum, g, mask, workspace)
     for name, t, dtype in (("w", w, torch.float32), ("momentum", momentum, torch.float32), ("g", g, g.dtype), ("mask", mask, torch.uint8)):
         if t is not None and (t.shape != w.shape or t.dtype != dtype or not t.is_contiguous()):
             raise ValueError(f"{name}: contiguous values of {dtype} with the weights' extents wanted")

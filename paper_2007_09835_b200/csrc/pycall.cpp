@@ -13,7 +13,7 @@
 namespace {
 
 PyObject *g_float32, *g_bfloat16, *g_raw_stream, *g_get_device;      // owned
-PyObject *s_shape, *s_stride, *s_dtype, *s_data_ptr;
+PyObject *s_shape, *s_stride, *s_dtype, *s_data_ptr, *s_get_device;
 
 typedef rt3d_status (*ConvFn)(const rt3d_tensor*, const rt3d_packed*, const float*, const rt3d_conv_params*, rt3d_tensor*, void*);
 typedef rt3d_status (*FusedFn)(const rt3d_tensor*, const rt3d_packed*, const float*, const rt3d_conv_params*,
@@ -256,17 +256,54 @@ bool structure(PyObject* v, S* out) {
   return ok;
 }
 
-// linear_w4(address, x, weights, bias, y, relu, stream) -> status
+// The number that a tensor's method without arguments answers, -1 with an exception set where it fails.
+long long number_of(PyObject* t, PyObject* method) {
+  PyObject* r = PyObject_CallMethodNoArgs(t, method);
+  if (!r) return -1;
+  const long long v = PyLong_AsLongLong(r);
+  Py_DECREF(r);
+  return v;
+}
+// Refuses a tensor that is not on the weights' device (a kernel would read host memory, or another device's), -1 for the host.
+bool on_device(PyObject* t, long device) {
+  const long long d = number_of(t, s_get_device);
+  if (d == -1 && PyErr_Occurred()) return false;
+  if (d >= 0 && d == device) return true;
+  PyErr_Format(PyExc_ValueError, "a tensor on CUDA device %ld wanted, where the weights are (-1: the host); it is on %lld", device, d);
+  return false;
+}
+// The weights' device has to be the current one, on which the call is launched.
+bool on_current_device(PyObject* index, long* device) {
+  *device = PyLong_AsLong(index);
+  if (*device == -1 && PyErr_Occurred()) return false;
+  if (*device < 0) {
+    PyErr_SetString(PyExc_ValueError, "the weights are in host memory");
+    return false;
+  }
+  PyObject* r = PyObject_CallNoArgs(g_get_device);
+  if (!r) return false;
+  const long now = PyLong_AsLong(r);
+  Py_DECREF(r);
+  if (now == -1 && PyErr_Occurred()) return false;
+  if (now == *device) return true;
+  PyErr_Format(PyExc_ValueError, "the weights are on CUDA device %ld, the current one is %ld", *device, now);
+  return false;
+}
+
+// linear_w4(address, x, weights, their device, bias, y, relu, stream) -> status
 PyObject* linear_w4(PyObject*, PyObject* const* a, Py_ssize_t n) {
   uintptr_t fn, bias, stream;
   rt3d_tensor x{}, y{};
   rt3d_w4 q;
-  if (!want(n, 7) || !as_pointer(a[0], &fn) || !structure(a[2], &q) || !tensor_or_none(a[3], &bias)) return nullptr;
+  long device;
+  if (!want(n, 8) || !as_pointer(a[0], &fn) || !structure(a[2], &q) || !on_current_device(a[3], &device) || !on_device(a[1], device) ||
+      !on_device(a[5], device) || (a[4] != Py_None && !on_device(a[4], device)) || !tensor_or_none(a[4], &bias))
+    return nullptr;
   PyObject *k = PyLong_FromLong(q.k), *m = PyLong_FromLong(q.m);
-  const bool ok = k && m && describe(a[1], k, &x) && describe(a[4], m, &y);
+  const bool ok = k && m && describe(a[1], k, &x) && describe(a[5], m, &y);
   Py_XDECREF(k); Py_XDECREF(m);
-  const int relu = ok ? PyObject_IsTrue(a[5]) : -1;
-  if (relu < 0 || !stream_of(a[6], &stream)) return nullptr;
+  const int relu = ok ? PyObject_IsTrue(a[6]) : -1;
+  if (relu < 0 || !stream_of(a[7], &stream)) return nullptr;
   return released([&] {
     return reinterpret_cast<decltype(&rt3d_linear_w4)>(fn)(&x, &q, reinterpret_cast<const float*>(bias), relu, &y, reinterpret_cast<void*>(stream));
   });
@@ -304,13 +341,16 @@ bool matrix(PyObject* t, int64_t m, int64_t k, uintptr_t* data, int* dtype, int6
   return *dtype >= 0 && data_ptr(t, data);
 }
 
-// w4_quantize(address, weights, w, stream) and w4_unpack(address, weights, w, stream) -> status
+// w4_quantize(address, weights, their device, w, stream) and w4_unpack with the same arguments -> status
 PyObject* w4_quantize(PyObject*, PyObject* const* a, Py_ssize_t n) {
   uintptr_t fn, w, stream;
   rt3d_w4 q;
   int dtype;
   int64_t pitch;
-  if (!want(n, 4) || !as_pointer(a[0], &fn) || !structure(a[1], &q) || !matrix(a[2], q.m, q.k, &w, &dtype, &pitch) || !stream_of(a[3], &stream)) return nullptr;
+  long device;
+  if (!want(n, 5) || !as_pointer(a[0], &fn) || !structure(a[1], &q) || !on_current_device(a[2], &device) || !on_device(a[3], device) ||
+      !matrix(a[3], q.m, q.k, &w, &dtype, &pitch) || !stream_of(a[4], &stream))
+    return nullptr;
   return released([&] {
     return reinterpret_cast<decltype(&rt3d_w4_quantize)>(fn)(reinterpret_cast<const void*>(w), dtype, pitch, &q, reinterpret_cast<void*>(stream));
   });
@@ -320,7 +360,10 @@ PyObject* w4_unpack(PyObject*, PyObject* const* a, Py_ssize_t n) {
   rt3d_w4 q;
   int dtype;
   int64_t pitch;
-  if (!want(n, 4) || !as_pointer(a[0], &fn) || !structure(a[1], &q) || !matrix(a[2], q.m, q.k, &w, &dtype, &pitch) || !stream_of(a[3], &stream)) return nullptr;
+  long device;
+  if (!want(n, 5) || !as_pointer(a[0], &fn) || !structure(a[1], &q) || !on_current_device(a[2], &device) || !on_device(a[3], device) ||
+      !matrix(a[3], q.m, q.k, &w, &dtype, &pitch) || !stream_of(a[4], &stream))
+    return nullptr;
   return released([&] {
     return reinterpret_cast<decltype(&rt3d_w4_unpack)>(fn)(&q, dtype, reinterpret_cast<void*>(w), pitch, reinterpret_cast<void*>(stream));
   });
@@ -334,7 +377,7 @@ PyMethodDef methods[] = {
     {"reweight", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(reweight)), METH_FASTCALL, ""},
     {"expand_mask", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(expand_mask)), METH_FASTCALL, ""},
     {"linear_w4", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(linear_w4)), METH_FASTCALL,
-     "linear_w4(address, x, weights, bias, y, relu, stream) -> status"},
+     "linear_w4(address, x, weights, their device, bias, y, relu, stream) -> status"},
     {"w4_quantize", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(w4_quantize)), METH_FASTCALL, ""},
     {"w4_unpack", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(w4_unpack)), METH_FASTCALL, ""},
     {"pointers_are", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(pointers_are)), METH_FASTCALL,
@@ -350,5 +393,6 @@ PyMODINIT_FUNC PyInit__pycall(void) {
   s_stride = PyUnicode_InternFromString("stride");
   s_dtype = PyUnicode_InternFromString("dtype");
   s_data_ptr = PyUnicode_InternFromString("data_ptr");
+  s_get_device = PyUnicode_InternFromString("get_device");
   return PyModule_Create(&module);
 }

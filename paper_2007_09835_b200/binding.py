@@ -669,6 +669,9 @@ def rt3d_linear_w4(x, q: W4Weights, bias, y, relu=False, stream=None):
         if status != OK:
             raise Rt3dError(status, "rt3d_linear_w4")
         return
+    import torch
+    if bias is not None and (bias.dtype != torch.float32 or bias.numel() != q.m or not bias.is_contiguous()):
+        raise ValueError(f"bias: {q.m} contiguous float32 values wanted")
     _on_device(q.index, bias, *(t for t in (x, y) if not isinstance(t, Tensor)))
     xd = x if isinstance(x, Tensor) else tensor_desc(x, q.k)
     yd = y if isinstance(y, Tensor) else tensor_desc(y, q.m)

@@ -7,13 +7,14 @@
 #include <Python.h>
 
 #include <cstdint>
+#include <initializer_list>
 
 #include "rt3d.h"
 
 namespace {
 
 PyObject *g_float32, *g_bfloat16, *g_raw_stream, *g_get_device;      // owned
-PyObject *s_shape, *s_stride, *s_dtype, *s_data_ptr, *s_get_device;
+PyObject *s_shape, *s_stride, *s_dtype, *s_data_ptr, *s_get_device, *s_numel, *s_is_contiguous;
 
 typedef rt3d_status (*ConvFn)(const rt3d_tensor*, const rt3d_packed*, const float*, const rt3d_conv_params*, rt3d_tensor*, void*);
 typedef rt3d_status (*FusedFn)(const rt3d_tensor*, const rt3d_packed*, const float*, const rt3d_conv_params*,
@@ -290,6 +291,27 @@ bool on_current_device(PyObject* index, long* device) {
   return false;
 }
 
+// A bias of m contiguous float32 values, or None: fewer or others would be read past their end.
+bool bias_of(PyObject* t, long long m, long device, uintptr_t* out) {
+  *out = 0;
+  if (t == Py_None) return true;
+  if (!on_device(t, device)) return false;
+  PyObject* dt = PyObject_GetAttr(t, s_dtype);
+  if (!dt) return false;
+  bool ok = dt == g_float32;
+  Py_DECREF(dt);
+  for (PyObject* method : {s_numel, s_is_contiguous}) {
+    const long long v = number_of(t, method);
+    if (v == -1 && PyErr_Occurred()) return false;
+    ok = ok && v == (method == s_numel ? m : 1);
+  }
+  if (!ok) {
+    PyErr_Format(PyExc_ValueError, "bias: %lld contiguous float32 values wanted", m);
+    return false;
+  }
+  return data_ptr(t, out);
+}
+
 // linear_w4(address, x, weights, their device, bias, y, relu, stream) -> status
 PyObject* linear_w4(PyObject*, PyObject* const* a, Py_ssize_t n) {
   uintptr_t fn, bias, stream;
@@ -297,7 +319,7 @@ PyObject* linear_w4(PyObject*, PyObject* const* a, Py_ssize_t n) {
   rt3d_w4 q;
   long device;
   if (!want(n, 8) || !as_pointer(a[0], &fn) || !structure(a[2], &q) || !on_current_device(a[3], &device) || !on_device(a[1], device) ||
-      !on_device(a[5], device) || (a[4] != Py_None && !on_device(a[4], device)) || !tensor_or_none(a[4], &bias))
+      !on_device(a[5], device) || !bias_of(a[4], q.m, device, &bias))
     return nullptr;
   PyObject *k = PyLong_FromLong(q.k), *m = PyLong_FromLong(q.m);
   const bool ok = k && m && describe(a[1], k, &x) && describe(a[5], m, &y);
@@ -394,5 +416,7 @@ PyMODINIT_FUNC PyInit__pycall(void) {
   s_dtype = PyUnicode_InternFromString("dtype");
   s_data_ptr = PyUnicode_InternFromString("data_ptr");
   s_get_device = PyUnicode_InternFromString("get_device");
+  s_numel = PyUnicode_InternFromString("numel");
+  s_is_contiguous = PyUnicode_InternFromString("is_contiguous");
   return PyModule_Create(&module);
 }

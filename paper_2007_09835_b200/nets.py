@@ -160,6 +160,8 @@ class LinearW4Layer:
             self.quantize(w)
         if bias is not None and not isinstance(bias, torch.Tensor):
             bias = torch.from_numpy(np.ascontiguousarray(bias, np.float32))
+        if bias is not None and bias.numel() != spec.cout:
+            raise ValueError("a bias of one value for each filter wanted")
         self.bias = None if bias is None else bias.to(device=device, dtype=torch.float32).contiguous()
 
     def quantize(self, w, stream=None):

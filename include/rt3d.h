@@ -377,7 +377,7 @@ int64_t rt3d_w4_scale_count(int m, int k, int group);
  * What x holds behind its last channel does not matter; y's padding channels are left as they are.  The result of a row
  * does not depend on timing; it may depend, within rounding, on how many rows the call has.
  * All enqueue on `stream`, allocate nothing and do not synchronise.  Errors: INVALID_ARG, SHAPE, UNSUPPORTED (a device that
- * is not of compute capability 10.x; 2^31 rows or tiles of codes and more, more than 2^30 inputs), CUDA. */
+ * is not of compute capability 10.x; 2^31 rows or tiles of codes and more, more than 2^31 - 64 filters or 2^30 inputs), CUDA. */
 rt3d_status rt3d_w4_quantize(const void* w, int dtype, int64_t pitch, const rt3d_w4* q, void* stream);
 rt3d_status rt3d_w4_unpack(const rt3d_w4* q, int dtype, void* w, int64_t pitch, void* stream);
 rt3d_status rt3d_linear_w4(const rt3d_tensor* x, const rt3d_w4* q, const float* bias, int relu, rt3d_tensor* y, void* stream);

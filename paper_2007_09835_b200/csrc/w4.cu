@@ -579,8 +579,8 @@ linear_w4_kernel(const LinearArgs a) {
 }
 
 bool valid_extents(int64_t m, int64_t k) { return m > 0 && k > 0; }
-// Tiles of codes are counted, and inputs addressed, in 32 bits.
-bool small_enough(int64_t m, int64_t k) { return k <= (1 << 30) && ceil_div64(m, 16) * ceil_div64(k, 64) < (int64_t(1) << 31); }
+// Tiles of codes are counted, and filters (up to whole tiles) and inputs addressed, in 32 bits.
+bool small_enough(int64_t m, int64_t k) { return m <= (int64_t(1) << 31) - 64 && k <= (1 << 30) && ceil_div64(m, 16) * ceil_div64(k, 64) < (int64_t(1) << 31); }
 bool valid_group(int group) { return group == 32 || group == 64 || group == 128; }
 
 rt3d_status check_w4(const rt3d_w4* q) {

@@ -106,6 +106,25 @@ EncodeTiledFn g_encode = nullptr;
 typedef CUresult (*ReplaceAddressFn)(CUtensorMap*, void*);
 ReplaceAddressFn g_replace_address = nullptr;
 
+// The words of DeviceState::sched, zeroed.  The library's first call on a device may be one that is being captured, which allocation
+// and legacy-stream work would end: both happen in the relaxed mode and on a stream of their own, outside of the capture.
+rt3d_status make_sched(int32_t** out) {
+  cudaStreamCaptureMode mode = cudaStreamCaptureModeRelaxed;
+  if (cudaThreadExchangeStreamCaptureMode(&mode) != cudaSuccess) return RT3D_ERR_CUDA;
+  int32_t* words = nullptr;
+  cudaStream_t st = nullptr;
+  rt3d_status s = RT3D_OK;
+  if (dev_malloc(&words, 256 * sizeof(int32_t)) != cudaSuccess) s = RT3D_ERR_ALLOC;
+  else if (cudaStreamCreateWithFlags(&st, cudaStreamNonBlocking) != cudaSuccess || cudaMemsetAsync(words, 0, 256 * sizeof(int32_t), st) != cudaSuccess ||
+           cudaStreamSynchronize(st) != cudaSuccess)
+    s = RT3D_ERR_CUDA;
+  if (st) cudaStreamDestroy(st);
+  if (s != RT3D_OK && words) cudaFree(words);
+  cudaThreadExchangeStreamCaptureMode(&mode);
+  if (s == RT3D_OK) *out = words;
+  return s;
+}
+
 rt3d_status get_device_state(DeviceState** out) {
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return RT3D_ERR_CUDA;
@@ -114,8 +133,8 @@ rt3d_status get_device_state(DeviceState** out) {
   if (!d.init) {
     if (cudaDeviceGetAttribute(&d.sm_count, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return RT3D_ERR_CUDA;
     if (cudaDeviceGetAttribute(&d.cc_major, cudaDevAttrComputeCapabilityMajor, dev) != cudaSuccess) return RT3D_ERR_CUDA;
-    if (dev_malloc(&d.sched, 256 * sizeof(int32_t)) != cudaSuccess) return RT3D_ERR_ALLOC;
-    if (cudaMemset(d.sched, 0, 256 * sizeof(int32_t)) != cudaSuccess || uploads_done() != cudaSuccess) return RT3D_ERR_CUDA;
+    const rt3d_status made = make_sched(&d.sched);
+    if (made != RT3D_OK) return made;
     if (!g_encode) {
       void* fn = nullptr;
       cudaDriverEntryPointQueryResult qres;

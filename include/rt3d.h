@@ -406,7 +406,7 @@ rt3d_status rt3d_linear_w4(const rt3d_tensor* x, const rt3d_w4* q, const float* 
  *   value of [0, 1] below 1.9 in every step and |a + b s + c s s| at most 50, else UNSUPPORTED.  eps > 0.  p NULL: 5 steps, eps 1e-7.
  * rt3d_ortho_workspace: bytes of the workspace both calls need (16-byte aligned, caller-owned, contents of no meaning between
  *   calls; two calls that may overlap on the GPU, or two captured graphs that may, need one each); -1 for m or k < 1 or too large.
- *   No array of a call may overlap another one of it, except that momentum and w are updated in place.
+ *   No array of a call may overlap another one of it (INVALID_ARG); momentum and w are updated in place.
  * Both enqueue on `stream`, allocate nothing and do not synchronise.  The same inputs give the same bits.
  * Errors: INVALID_ARG, WORKSPACE (too few bytes), UNSUPPORTED (compute capability other than 10.x, coefficients), CUDA.
  */

@@ -18,6 +18,7 @@
 #include <cmath>
 #include <cstdint>
 #include <cstring>
+#include <initializer_list>
 
 #include "pdl.cuh"
 #include "rt3d.h"
@@ -1291,6 +1292,17 @@ rt3d_status direction(const Source<T>& src, int m, int k, const Plan& plan, cons
   return RT3D_OK;
 }
 
+// Whether any two of a call's arrays share memory.
+struct Area { const void* at; int64_t bytes; };
+bool any_overlap(std::initializer_list<Area> areas) {
+  for (const Area* a = areas.begin(); a != areas.end(); ++a)
+    for (const Area* b = areas.begin(); b != a; ++b) {
+      const uintptr_t a0 = reinterpret_cast<uintptr_t>(a->at), b0 = reinterpret_cast<uintptr_t>(b->at);
+      if (a->at && b->at && a0 < b0 + uintptr_t(b->bytes) && b0 < a0 + uintptr_t(a->bytes)) return true;
+    }
+  return false;
+}
+
 rt3d_status check_call(const void* g, int dtype, int m, int k, void* workspace, int64_t bytes) {
   if (!g || !workspace || m < 1 || k < 1 || (dtype != RT3D_F32 && dtype != RT3D_BF16)) return RT3D_ERR_INVALID_ARG;
   if (reinterpret_cast<uintptr_t>(g) % (dtype == RT3D_BF16 ? 2 : 4) || reinterpret_cast<uintptr_t>(workspace) % 16) return RT3D_ERR_INVALID_ARG;
@@ -1336,9 +1348,8 @@ rt3d_status rt3d_orthogonalize(const void* g, int dtype, int64_t g_pitch, int m,
   rt3d_status s = check_call(g, dtype, m, k, workspace, workspace_bytes);
   if (s != RT3D_OK) return s;
   if (!out || reinterpret_cast<uintptr_t>(out) % 2 || g_pitch < k || out_pitch < k) return RT3D_ERR_INVALID_ARG;
-  const char *g0 = static_cast<const char*>(g), *o0 = static_cast<const char*>(out);
   const int64_t size = dtype == RT3D_BF16 ? 2 : 4;
-  if (g0 < o0 + ((m - 1) * out_pitch + k) * 2 && o0 < g0 + ((m - 1) * g_pitch + k) * size) return RT3D_ERR_INVALID_ARG;
+  if (any_overlap({{g, ((m - 1) * g_pitch + k) * size}, {out, ((m - 1) * out_pitch + k) * 2}, {workspace, rt3d_ortho_workspace(m, k)}})) return RT3D_ERR_INVALID_ARG;
   if ((s = make_plan(p, &plan)) != RT3D_OK || plan_only()) return s;
   DeviceInfo dev;
   if ((s = current_device_info(&dev)) != RT3D_OK) return s;
@@ -1356,13 +1367,9 @@ rt3d_status rt3d_ortho_update(float* w, float* momentum, const void* g, int dtyp
   rt3d_status s = check_call(g, dtype, m, k, workspace, workspace_bytes);
   if (s != RT3D_OK) return s;
   if (!w || !momentum || !p || reinterpret_cast<uintptr_t>(w) % 4 || reinterpret_cast<uintptr_t>(momentum) % 4) return RT3D_ERR_INVALID_ARG;
-  const struct { const void* at; int64_t bytes; } area[3] = {{w, 4}, {momentum, 4}, {g, dtype == RT3D_BF16 ? 2 : 4}};
-  for (int i = 0; i < 3; ++i)
-    for (int j = 0; j < i; ++j) {
-      const char *a = static_cast<const char*>(area[i].at), *b = static_cast<const char*>(area[j].at);
-      const int64_t count = int64_t(m) * k;
-      if (a < b + count * area[j].bytes && b < a + count * area[i].bytes) return RT3D_ERR_INVALID_ARG;
-    }
+  const int64_t count = int64_t(m) * k;
+  if (any_overlap({{w, 4 * count}, {momentum, 4 * count}, {g, (dtype == RT3D_BF16 ? 2 : 4) * count}, {mask, count}, {workspace, rt3d_ortho_workspace(m, k)}}))
+    return RT3D_ERR_INVALID_ARG;
   if (!std::isfinite(p->lr) || !std::isfinite(p->mu) || !std::isfinite(p->weight_decay) || !std::isfinite(p->scale)) return RT3D_ERR_INVALID_ARG;
   if ((s = make_plan(&p->ortho, &plan)) != RT3D_OK || plan_only()) return s;
   DeviceInfo dev;

@@ -376,8 +376,9 @@ int64_t rt3d_w4_scale_count(int m, int k, int group);
  * and a group's sum is multiplied by its scale, all in fp32: nothing is rounded but the sums, and bf16 outputs once at the end.
  * What x holds behind its last channel does not matter; y's padding channels are left as they are.  The result of a row
  * does not depend on timing; it may depend, within rounding, on how many rows the call has.
- * All enqueue on `stream`, allocate nothing and do not synchronise.  Errors: INVALID_ARG, SHAPE, UNSUPPORTED (a device that
- * is not of compute capability 10.x; 2^31 rows or tiles of codes and more, more than 2^31 - 64 filters or 2^30 inputs), CUDA. */
+ * fp32 values of x enter as three bf16 parts, which hold all 24 bits down to 2^-110 in magnitude; of smaller ones, what lies under 2^-133 is lost.
+ * All enqueue on `stream`, allocate nothing and do not synchronise.  Errors: INVALID_ARG, SHAPE, UNSUPPORTED (2^31 rows or tiles of
+ * codes and more, more than 2^31 - 64 filters or 2^30 inputs; rt3d_linear_w4: a device that is not of compute capability 10.x), CUDA. */
 rt3d_status rt3d_w4_quantize(const void* w, int dtype, int64_t pitch, const rt3d_w4* q, void* stream);
 rt3d_status rt3d_w4_unpack(const rt3d_w4* q, int dtype, void* w, int64_t pitch, void* stream);
 rt3d_status rt3d_linear_w4(const rt3d_tensor* x, const rt3d_w4* q, const float* bias, int relu, rt3d_tensor* y, void* stream);
@@ -408,6 +409,8 @@ rt3d_status rt3d_linear_w4(const rt3d_tensor* x, const rt3d_w4* q, const float* 
  *   calls; two calls that may overlap on the GPU, or two captured graphs that may, need one each); -1 for m or k < 1 or too large.
  *   No array of a call may overlap another one of it (INVALID_ARG); momentum and w are updated in place.
  * Both enqueue on `stream`, allocate nothing and do not synchronise.  The same inputs give the same bits.
+ * A call that returns CUDA may have enqueued a part of its launches: rt3d_ortho_update brings the momentum up to date in the first of
+ * them and the weights in the last, so after that status both are to be taken from a copy, not to be updated again.
  * Errors: INVALID_ARG, WORKSPACE (too few bytes), UNSUPPORTED (compute capability other than 10.x, coefficients), CUDA.
  */
 typedef struct {

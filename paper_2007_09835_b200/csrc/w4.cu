@@ -258,7 +258,6 @@ w4_unpack_kernel(T* __restrict__ w, const GridArgs a) {
 // A CTA's eight warps take every eighth block of 64 inputs of kTiles tiles of filters; where there are few tiles, the CTAs of a cluster
 // share the inputs further and add their sums up through one another's shared memory, always in the same order.
 constexpr int kLinearThreads = 256;
-constexpr int kMostRows = 1 << 19;                          // of a launch
 // More rows go to linear_w4_many_rows.  4096 x 8192, us: 16 bf16 rows 11.2 here and 14 there, 32 rows 20 and 14; 16 fp32 rows 34 and 35.5, 64
 // rows 126 and 37.
 constexpr int kManyRows = 16;

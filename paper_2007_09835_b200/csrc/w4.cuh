@@ -22,7 +22,9 @@ struct LinearArgs {
   int rows;
 };
 
-// Many rows (w4_umma.cu), at most 2^22.
+// Many rows (w4_umma.cu), at most kMostRows: tiles of 64 rows are the grid's second extent.
+constexpr int kMostRows = 1 << 19;
+static_assert(kMostRows / 64 <= 65535, "tiles of 64 rows");
 rt3d_status linear_w4_many_rows(const LinearArgs& a, int dtype, const DeviceInfo& dev, cudaStream_t st);
 
 namespace {

@@ -4,12 +4,14 @@
 // first A, which commute and are symmetric.  So a few steps are taken on the small n x n matrices (n the shorter side, l the longer)
 //     G = X X^T;   P_1 = p_1(G), G <- P_1 G P_1, P_2 = p_2(G), ..;   Q = .. P_2 P_1;   X <- Q X
 // which reads X twice for up to three steps instead of twice a step, and of a symmetric product only the tiles on and under the
-// diagonal are computed.  Squaring X loses the small singular values s where s^2 falls under the rounding of G; with 22 bits of G and
-// at most three steps to a run (which enlarge by at most 41 = 3.4445^3) nothing of weight is lost: against 64 bits 4e-7 to 5e-6 of |O| for
-// matrices whose singular values fall off as 1 to 1/i^2, where five steps in one run give NaN.
+// diagonal are computed.  Squaring X loses the small singular values s where s^2 falls under the rounding of G; with 22 bits of G and at
+// most three steps to a run (which enlarge by at most 41 = 3.4445^3) little is lost: directions against 64 bits, of |O|, and fp32 products beside
+// them: noise of 64 x 576 6.9e-6 and 1.7e-6, 4096 x 8192 3.4e-5 and 7.2e-6; singular values as 1/i^2, 512 x 1024, 4.1e-5 and 2.5e-5; two
+// directions only, 2000 x 3000, 3.5e-4 and 1.3e-4.  (Five steps in one run give NaN.)
 // Values enter the tensor cores as fp16 parts, v = hi + lo (22 bits), products as hi hi + hi lo + lo hi with fp32 sums.  fp16's 11 bits
-// against bf16's 8, and a bf16 gradient is its own hi part.  (The X before the last steps without its lo part, for a result in bf16, leaves
-// 1.0e-3 of |O| beside that result's own rounding, 1.7e-3, in roundings that go the other way; it saved 3 to 16 %.)  Matrices are held times a power of two (2^14, 2^10 for P and Q) so that lo parts stay normal numbers.
+// against bf16's 8, and a bf16 gradient is its own hi part.  (The X before the last steps without its lo part, for a result in bf16,
+// left 1.0e-3 of |O| beside that result's own rounding of 1.7e-3; it saved 3 to 16 %.)  Matrices are held times a power of two (2^14,
+// 2^10 for P and Q) so that lo parts stay normal numbers.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
@@ -34,13 +36,17 @@ namespace {
 
 constexpr int kNormBlocks = 512;
 constexpr int kMostSteps = 16, kRuns = kMostSteps;
-// Up to this side the small matrices' products are steps of one launch.  A side of 512 against twice the length, five steps, us: as launches 162,
-// as steps 141; 768: 169 and 166; 1024: 308 and 214; 1280: 256 either way.
+// Up to this side the small matrices' products are steps of one launch.  A side of 512 against twice the length, five steps, us: as launches 154,
+// as steps 145; 768: 187 and 176; 1024: 215 and 214; 1280: 280 and 285.
 constexpr int kFusedSide = 1024;
-// Where X is short as well, everything is, with runs of one step, which need the fewest products in a row.  Side 64, us: 512 long 75 in
-// runs of three and 60 this way, 768: 75 and 71, 1024: 75 and 77; side 256: 512 100 and 83, 768 102 and 102; side 512: 1024 139 and 127,
-// 2048 142 and 154; side 768: 1536 165 and 157, three times the side 171 and 204; side 1024: 1536 211 and 209, 2048 214 and 221.
-constexpr bool everything_fused(int n, int l) { return n <= kFusedSide && (l <= 768 || (l <= 2 * n && l <= 1536)); }
+// Where X is short as well, everything is, with runs of one step, which need the fewest products in a row, as long as X's tiles of
+// 128 x 64 are one round of the SMs.  us, in runs of two and three and this way: side 64: 512 long 77 and 66, 768 79 and 74, 1024 79 and 82;
+// side 256: 512 99 and 80, 768 102 and 100, 1024 102 and 107; side 512: 1024 145 and 134, 2048 149 and 168; side 768: 768 171 and 146,
+// 1536 176 and 171 (144 tiles); side 896: 1344 190 and 174, 1536 191 and 211 (168 tiles); side 1024: 1024 199 and 172, 1280 207 and 218
+// (160 tiles), 1536 208 and 226.
+inline bool everything_fused(int n, int l, int sms) {
+  return n <= kFusedSide && (l <= 768 || (l <= 2 * n && l <= 1536 && ceil_div(n, 128) * ceil_div(l, 64) <= sms));
+}
 constexpr float kXScale = 16384.f, kGScale = 16384.f, kPScale = 1024.f;        // what X, G and T, P and Q are held times
 
 __device__ __forceinline__ float value_of(const float* p) { return *p; }
@@ -1182,7 +1188,7 @@ rt3d_status direction(const Source<T>& src, int m, int k, const Plan& plan, cons
   Runner r{dev, st, ws};
   if (!r.make_maps()) return RT3D_ERR_CUDA;
   const bool turned = m > k;
-  const bool short_x = turned ? everything_fused(k, m) : everything_fused(m, k);
+  const bool short_x = turned ? everything_fused(k, m, dev.sm_count) : everything_fused(m, k, dev.sm_count);
   uintptr_t bits = reinterpret_cast<uintptr_t>(src.g) | uintptr_t(src.pitch) * sizeof(T);       // 4 values at a time
   bool vec = k % 4 == 0 && bits % (4 * sizeof(T)) == 0;
   if (src.momentum) vec = vec && reinterpret_cast<uintptr_t>(src.momentum) % 16 == 0 && reinterpret_cast<uintptr_t>(src.mask) % 4 == 0;

@@ -258,8 +258,9 @@ w4_unpack_kernel(T* __restrict__ w, const GridArgs a) {
 // A CTA's eight warps take every eighth block of 64 inputs of kTiles tiles of filters; where there are few tiles, the CTAs of a cluster
 // share the inputs further and add their sums up through one another's shared memory, always in the same order.
 constexpr int kLinearThreads = 256;
-// More rows go to linear_w4_many_rows.  4096 x 8192, us: 16 bf16 rows 11.2 here and 14 there, 32 rows 20 and 14; 16 fp32 rows 34 and 35.5, 64
-// rows 126 and 37.
+// More rows go to linear_w4_many_rows.  us here and there, groups of 128: 4096 x 8192, bf16: 16 rows 10.8 and 13.7, 32 rows 16.3 and 13.8;
+// fp32: 16 rows 33.3 and 24.2, 64 rows 101 and 26 (groups of 32, 16 rows: 36.3 and 35.4).  487 x 4096, bf16: 16 rows 5.1 and 6.7, 32 rows 5.6
+// and 6.8; fp32: 16 rows 13.7 and 10.1.  One number for all: fp32 rows from 9 on would be faster there, 32 bf16 rows of narrow layers here.
 constexpr int kManyRows = 16;
 
 __device__ __forceinline__ void mma_bf16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
@@ -673,7 +674,7 @@ rt3d_status linear(const rt3d_tensor* x, const rt3d_w4* q, const float* bias, in
   const int rows8 = rows <= 8 ? 1 : 2;
   // tiles of a CTA at most: sixteen fp32 rows take three times the registers of bf16 ones
   const int most = rows8 == 2 && sizeof(T) == 4 ? 2 : 4;
-  // One CTA an SM for up to two tiles each (4096 x 8192, one row: 7.3 us as 256 CTAs, 7.3 as 148; 16 rows: 12.0 and 10.7), two for
+  // One CTA an SM for up to two tiles each (4096 x 8192, one row: 7.2 us as 256 CTAs and as 148; 16 rows: 11.9 and 11.0), two for
   // more (16384 x 16384, 4 rows: 37.4 us as 342 CTAs of up to 3 tiles, 30.3 as 296 of up to 4).  With fewer tiles than that, the CTAs
   // of a cluster share the inputs while every warp keeps eight blocks (16384 inputs of 1000 filters, one row: 7.9 us alone, 5.9
   // shared by four; 4096 inputs of 487: 4.0 alone, 4.2 by two).

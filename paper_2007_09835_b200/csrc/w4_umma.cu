@@ -6,8 +6,9 @@
 // one number), kCols rows of x their columns.  Eight warps turn codes into the bf16 operand (c - z) / 64 in shared memory, 128 filters x
 // 64 inputs a stage; x comes by TMA, which also makes zeros of what lies behind the last input and row.
 // A stage of 128 filters x 128 inputs x 128 rows writes 64 KB of shared memory and reads 64 KB, 1024 clocks at 128 bytes a clock, against 512
-// of the tensor cores; it takes 1600, the hand-overs between the warps (4096 x 8192, groups of 128: 64 rows 14 us, 128 rows 18, 256 rows 29,
-// 0.82 TB/s and 600 TFLOP/s; with groups of 32, four sums to a stage, 75).  fp32 rows: 64 37 us, 512 239, bound by the warps that split them.
+// of the tensor cores; it takes 1650, the hand-overs between the warps (4096 x 8192, groups of 128: 64 rows 14 us, 128 rows 18, 256 rows 29,
+// 0.82 TB/s and 600 TFLOP/s; with groups of 32, four sums to a stage, 75).  fp32 rows, bound by the warps that split them: 64 rows 26 us, with
+// groups of 32 38, 512 rows 240.
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>

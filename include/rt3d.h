@@ -397,11 +397,11 @@ rt3d_status rt3d_linear_w4(const rt3d_tensor* x, const rt3d_w4* q, const float* 
  *   mask uint8 (nonzero = kept, the form of rt3d_kgs_expand_mask) or NULL; where it is zero, w and momentum become zero whatever
  *   w, momentum and g hold there.
  * Products take two fp16 parts (22 bits) of every value on the tensor cores, with fp32 sums; rt3d_orthogonalize rounds the result to
- * bf16, once.  Before that a direction is off by at most 2^-19 S max(|O|, |X|) (Frobenius norms, sides up to 2^18, |X| = |g| / (|g| + eps)),
- * S the sum over the steps of (|a| + |b| + |c|) times the product of the later steps' largest |a + b s + c s s|: what is rounded
- * in directions of small singular values is enlarged like they are, 485 times by the usual five steps, 2e4 times by eight.  The usual five
- * steps keep 1e-4 |O| where the gradient has noise in all its directions; where it has a few directions only, 4e-4 were measured (fp32
- * products: 1.3e-4).
+ * bf16, once.  Before that a direction is off by at most 2^-18 S max(|O|, |X|) (Frobenius norms, sides up to 2^18, |X| = |g| / (|g| + eps)),
+ * S the sum over the steps of (|a| + 2 |b| + 4 |c|) times the product of the later steps' largest |a + b s + c s s|: what is rounded
+ * in directions of small singular values is enlarged like they are, 485 times by the usual five steps, 2e4 times by eight.  Most gradients
+ * stay far under it: the usual five steps keep 1e-4 |O| where there is noise in all directions (3e-6 to 4.4e-5 were measured); where there
+ * are a few directions only, up to 3.5e-4 were measured (fp32 products: 1.3e-4).
  * A gradient with an infinity or a NaN gives NaN (where the mask keeps anything), one of zeros gives zeros.
  *   steps 1..16; coefs HOST [steps][3] (a, b, c of each step) or NULL for 3.4445, -4.7750, 2.0315; they must keep every singular
  *   value of [0, 1] below 1.9 in every step and |a + b s + c s s| at most 50, else UNSUPPORTED.  eps > 0.  p NULL: 5 steps, eps 1e-7.

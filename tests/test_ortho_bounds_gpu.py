@@ -2,9 +2,12 @@
 
 The bound.  A value in two fp16 parts is off by at most 2^-23 of itself: the first leaves at most 2^-11 of it, of which the second has
 11 bits.  A product of two such values leaves out that of the second parts, 2^-22, and its result is held in two parts again:
-2 2^-23 + 2^-22 + 2^-23 = 0.63 2^-20 of what a step's |a| + |b| + |c| works on, and 2^-20 with what the sums round.  The later steps
-enlarge that by their largest |a + b s + c s s| where it lies in directions of small singular values.  So, of the Frobenius norm,
-2^-20 S max(|O|, |X|), S the sum over the steps of (|a| + |b| + |c|) times the later steps' largest |p|, |X| = |u| / (|u| + eps)."""
+2 2^-23 + 2^-22 + 2^-23 = 0.63 2^-20.  The tensor core cuts off what lies under the last bit of an accumulator, half a bit or 2^-24 of it
+on average; in a sum of one sign, over 512 inputs in 96 additions, that is 96 2^-24 of half the sum, 3.0 2^-20.  Together under 2^-18 for
+one product.  Of a step a X has one (P X), b A X two (A, P X), c A A X four (A twice, A A, P X).  The later steps enlarge what that
+leaves by their largest |a + b s + c s s| where it lies in directions of small singular values.  So, of the Frobenius norm,
+2^-18 S max(|O|, |X|), S the sum over the steps of (|a| + 2 |b| + 4 |c|) times the later steps' largest |p|, |X| = |u| / (|u| + eps).
+"""
 import numpy as np
 import pytest
 import torch
@@ -24,12 +27,12 @@ def enlargement(steps, coefs=None):
         p = a + b * s ** 2 + c * s ** 4
         most.append(np.abs(p).max())
         top = np.abs(s * p).max()
-    return sum(sum(map(abs, abc)) * np.prod(most[i + 1:]) for i, abc in enumerate(coefs))
+    return sum((abs(a) + 2 * abs(b) + 4 * abs(c)) * np.prod(most[i + 1:]) for i, (a, b, c) in enumerate(coefs))
 
 
 def allowed(o, u, steps=5, coefs=None, eps=1e-7):
     norm = u.double().norm().item()
-    return 2.0 ** -20 * enlargement(steps, coefs) * max(o.norm().item(), norm / (norm + eps))
+    return 2.0 ** -18 * enlargement(steps, coefs) * max(o.norm().item(), norm / (norm + eps))
 
 
 def workspace(m, k):
@@ -123,3 +126,10 @@ def test_directions_are_rounded_once(m, k):
     out = torch.empty(m, k, dtype=torch.bfloat16, device="cuda")
     rt3d.rt3d_orthogonalize(u, out, workspace(m, k))
     assert torch.equal(out, fp32_direction(u).to(torch.bfloat16))
+
+
+@pytest.mark.parametrize("m,k", [(329, 283), (366, 2759), (2003, 1357)])
+def test_one_step_on_values_of_one_sign(m, k):
+    """Where a step enlarges nothing, what the sums cut off is the most of it."""
+    for coefs in ([(0.3, 0.2, 0.1)], [(1.5, -0.5, 0.0)]):
+        check(noise(m, k).abs(), 1, coefs)

@@ -91,15 +91,22 @@ bool describe(PyObject* t, PyObject* channels, rt3d_tensor* d) {
   return true;
 }
 
+// The stream's handle, or the current stream's of device `dev`.
+bool stream_on(PyObject* v, PyObject* dev, uintptr_t* out) {
+  if (v != Py_None) return as_pointer(v, out);
+  PyObject* st = PyObject_CallOneArg(g_raw_stream, dev);
+  if (!st) return false;
+  const bool ok = as_pointer(st, out);
+  Py_DECREF(st);
+  return ok;
+}
+
 bool stream_of(PyObject* v, uintptr_t* out) {
   if (v != Py_None) return as_pointer(v, out);
   PyObject* dev = PyObject_CallNoArgs(g_get_device);
   if (!dev) return false;
-  PyObject* st = PyObject_CallOneArg(g_raw_stream, dev);
+  const bool ok = stream_on(v, dev, out);
   Py_DECREF(dev);
-  if (!st) return false;
-  const bool ok = as_pointer(st, out);
-  Py_DECREF(st);
   return ok;
 }
 
@@ -325,7 +332,7 @@ PyObject* linear_w4(PyObject*, PyObject* const* a, Py_ssize_t n) {
   const bool ok = k && m && describe(a[1], k, &x) && describe(a[5], m, &y);
   Py_XDECREF(k); Py_XDECREF(m);
   const int relu = ok ? PyObject_IsTrue(a[6]) : -1;
-  if (relu < 0 || !stream_of(a[7], &stream)) return nullptr;
+  if (relu < 0 || !stream_on(a[7], a[3], &stream)) return nullptr;
   return released([&] {
     return reinterpret_cast<decltype(&rt3d_linear_w4)>(fn)(&x, &q, reinterpret_cast<const float*>(bias), relu, &y, reinterpret_cast<void*>(stream));
   });
@@ -371,7 +378,7 @@ PyObject* w4_quantize(PyObject*, PyObject* const* a, Py_ssize_t n) {
   int64_t pitch;
   long device;
   if (!want(n, 5) || !as_pointer(a[0], &fn) || !structure(a[1], &q) || !on_current_device(a[2], &device) || !on_device(a[3], device) ||
-      !matrix(a[3], q.m, q.k, &w, &dtype, &pitch) || !stream_of(a[4], &stream))
+      !matrix(a[3], q.m, q.k, &w, &dtype, &pitch) || !stream_on(a[4], a[2], &stream))
     return nullptr;
   return released([&] {
     return reinterpret_cast<decltype(&rt3d_w4_quantize)>(fn)(reinterpret_cast<const void*>(w), dtype, pitch, &q, reinterpret_cast<void*>(stream));
@@ -384,7 +391,7 @@ PyObject* w4_unpack(PyObject*, PyObject* const* a, Py_ssize_t n) {
   int64_t pitch;
   long device;
   if (!want(n, 5) || !as_pointer(a[0], &fn) || !structure(a[1], &q) || !on_current_device(a[2], &device) || !on_device(a[3], device) ||
-      !matrix(a[3], q.m, q.k, &w, &dtype, &pitch) || !stream_of(a[4], &stream))
+      !matrix(a[3], q.m, q.k, &w, &dtype, &pitch) || !stream_on(a[4], a[2], &stream))
     return nullptr;
   return released([&] {
     return reinterpret_cast<decltype(&rt3d_w4_unpack)>(fn)(&q, dtype, reinterpret_cast<void*>(w), pitch, reinterpret_cast<void*>(stream));
